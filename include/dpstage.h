@@ -633,6 +633,42 @@ dp_status dp_op_cross_attention_bwd(int32_t dtype, int32_t B, int32_t Sq, int32_
                                     const void *d_o, void *dq, void *dkv, void *ws, const dp_dropout *drop,
                                     void *hip_stream);
 
+/* Queries and keys between their projection and the attention: a norm of every head's vector and
+ * the token's rotary position, in one pass.  q has q_heads and k has kv_heads heads of head_dim
+ * elements a row, head h at column h*head_dim, rows ldq_in (ldk_in) elements apart, so both may be
+ * column blocks of one packed projection; the results go to rows ldq_out (ldk_out) apart.  For
+ * every head's vector x:
+ *   n = gain * x / sqrt(mean(x^2) + eps)  (q_gain, k_gain: [head_dim], NULL: n = x)
+ *   the first rot_dim elements of n are turned, pair i by the angle position * inv_freq[i]
+ *   (inv_freq: fp32 [rot_dim/2]): (a, b) -> scale * (a cos - b sin, b cos + a sin), where (a, b) is
+ *   (n[i], n[i + rot_dim/2]), or (n[2i], n[2i+1]) with interleaved = 1; the others stay.
+ * positions: int32 [rows], any values, or NULL: row % seq.  The angle is taken in 64 bits, so far
+ * positions keep their fraction of a turn; what stretches positions for a longer context goes into
+ * inv_freq and scale (1 for none).  Statistics and angles fp32, results rounded once.
+ * The backward takes dq_out, dk_out (the gradient of the results, rows as those) and q, k (needed
+ * where there is a gain; else may be NULL) and writes dq, dk (rows as q, k) and dq_gain, dk_gain
+ * (dtype, [head_dim], overwritten; not touched where the gain is NULL).  ws: device workspace of
+ * dp_op_qk_rotary_workspace_bytes bytes, for gains' gradients only.
+ * q_out may be q and dq may be dq_out (the same rows), k likewise; no other overlap.  head_dim is
+ * even and at most 1024 (DP_E_UNSUPPORTED otherwise).  Any alignment: 16-byte accesses where
+ * head_dim and rot_dim are multiples of 16, strides of 8 and pointers 16-byte aligned, element by
+ * element otherwise.  No rows: nothing is read, gains' gradients become zero.  Heads of one kind
+ * only: the other count 0, its pointers NULL. */
+typedef struct {
+  int32_t rows, seq, q_heads, kv_heads, head_dim, rot_dim, interleaved;
+  float eps, scale;
+  int64_t ldq_in, ldk_in, ldq_out, ldk_out;
+} dp_qk_rotary;
+size_t dp_op_qk_rotary_workspace_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+dp_status dp_op_qk_rotary_fwd(int32_t dtype, const dp_qk_rotary *shape, const void *q, const void *k,
+                              const void *q_gain /*nullable*/, const void *k_gain /*nullable*/, const float *inv_freq,
+                              const int32_t *positions /*nullable*/, void *q_out, void *k_out, void *hip_stream);
+dp_status dp_op_qk_rotary_bwd(int32_t dtype, const dp_qk_rotary *shape, const void *dq_out, const void *dk_out,
+                              const void *q, const void *k, const void *q_gain /*nullable*/,
+                              const void *k_gain /*nullable*/, const float *inv_freq,
+                              const int32_t *positions /*nullable*/, void *dq, void *dk, void *dq_gain, void *dk_gain,
+                              void *ws, void *hip_stream);
+
 /* Diagnostic for reading the roofline: the rate at which the matrix cores issue
  * v_mfma_f32_32x32x16_bf16 when nothing else limits them (operands in registers, 16
  * independent accumulators a wave, one workgroup a CU, `iters` rounds), with the operand bits

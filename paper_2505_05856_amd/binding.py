@@ -111,6 +111,13 @@ class MemoptReport(C.Structure):
         return {n: getattr(self, n) for n, _ in self._fields_}
 
 
+class QkRotary(C.Structure):
+    """dp_qk_rotary."""
+    _fields_ = [(n, C.c_int32) for n in ("rows", "seq", "q_heads", "kv_heads", "head_dim", "rot_dim", "interleaved")] + \
+               [("eps", C.c_float), ("scale", C.c_float)] + \
+               [(n, C.c_int64) for n in ("ldq_in", "ldk_in", "ldq_out", "ldk_out")]
+
+
 MEMOPT_VALIDATE = 1
 
 _lib = None
@@ -168,6 +175,10 @@ def lib() -> C.CDLL:
     L.dp_op_attention_dropout_bwd.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     L.dp_op_cross_attention_fwd.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
     L.dp_op_cross_attention_bwd.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.dp_op_qk_rotary_workspace_bytes.restype = sz
+    L.dp_op_qk_rotary_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    L.dp_op_qk_rotary_fwd.argtypes = [i32, C.POINTER(QkRotary)] + [vp] * 9
+    L.dp_op_qk_rotary_bwd.argtypes = [i32, C.POINTER(QkRotary)] + [vp] * 14
     L.dp_partition.argtypes = [C.POINTER(StageConfig), C.POINTER(CostModel), i32, u64, u64, u64, C.POINTER(C.c_int64),
                                C.POINTER(u64), C.c_uint32, C.POINTER(i32), vp, sz, C.POINTER(PartitionStage),
                                C.POINTER(PartitionReport)]
@@ -181,7 +192,7 @@ def lib() -> C.CDLL:
                  "dp_op_gelu_fwd", "dp_op_gelu_bwd", "dp_op_gemm", "dp_op_gemm_tile", "dp_op_linear_bwd", "dp_op_linear_bwd_tiles", "dp_op_colsum", "dp_op_colsum_static", "dp_op_attention_fwd",
                  "dp_op_attention_bwd", "dp_op_dropout", "dp_op_attention_dropout_fwd", "dp_op_attention_dropout_bwd",
                  "dp_op_cross_attention_fwd", "dp_op_cross_attention_bwd",
-                 "dp_op_rmsnorm_fwd", "dp_op_rmsnorm_bwd"):
+                 "dp_op_rmsnorm_fwd", "dp_op_rmsnorm_bwd", "dp_op_qk_rotary_fwd", "dp_op_qk_rotary_bwd"):
         getattr(L, name).restype = i32
     _lib = L
     return L
@@ -556,6 +567,89 @@ def op_cross_attention_bwd(q, kv, o, lse, d_o, B, Sq, Sk, nh, dh, dq, dkv, ws, d
     _check(lib().dp_op_cross_attention_bwd(_dt(q), B, Sq, Sk, nh, dh, _ptr(q), _ptr(kv), _ptr(o), _ptr(lse), _ptr(d_o),
                                            _ptr(dq), _ptr(dkv), _ptr(ws),
                                            C.byref(drop) if drop is not None else None, _stream_ptr(stream)))
+
+
+def _bad(text: str):
+    raise DpError(-1, text)
+
+
+def _heads(name, t, dt, device, rows=None, heads=None, dim=None):
+    """[rows, heads, head_dim] with whole heads side by side (a column block of a packed tensor is one): its row stride.  What the
+    library cannot see from a pointer is checked here: element type, shape, the inner strides, the device."""
+    if t.dim() != 3 or t.dtype != dt:
+        _bad(f"{name}: a tensor [rows, heads, head_dim] of {dt} is expected, got {tuple(t.shape)} of {t.dtype}")
+    n, h, d = t.shape
+    if (rows is not None and n != rows) or (heads is not None and h != heads) or (dim is not None and d != dim):
+        _bad(f"{name}: shape {tuple(t.shape)} does not match ({rows}, {heads}, {dim})")
+    s = t.stride()
+    if (d > 1 and s[2] != 1) or (h > 1 and s[1] != d):
+        _bad(f"{name}: the heads of a row must lie side by side (strides {s})")
+    if t.device != device:
+        _bad(f"{name}: on {t.device}, the call is for {device}")
+    return s[0] if n > 1 else max(s[0], h * d)
+
+
+def _vector(name, t, dt, device, n, optional=True):
+    if t is None:
+        if not optional:
+            _bad(f"{name} is missing")
+        return
+    if t.numel() != n or t.dtype != dt or not t.is_contiguous() or t.device != device:
+        _bad(f"{name}: {n} contiguous elements of {dt} on {device} are expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+
+
+def _call_device(t):
+    """The device of a call's tensors, which must be the current one (kernels go to the current device's stream)."""
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _bad(f"tensors on {t.device}: the operators work on the current device")
+    return t.device
+
+
+def _rotary_shape(q, k, q_out, k_out, q_gain, k_gain, inv_freq, positions, seq, interleaved, eps, scale):
+    import torch
+    dev, (T, nq, dh) = _call_device(q), q.shape if q.dim() == 3 else (-1, -1, -1)
+    lq = _heads("q", q, q.dtype, dev)
+    lk = _heads("k", k, q.dtype, dev, T, None, dh)
+    nk = k.shape[1]
+    lqo, lko = _heads("q_out", q_out, q.dtype, dev, T, nq, dh), _heads("k_out", k_out, q.dtype, dev, T, nk, dh)
+    _vector("q_gain", q_gain, q.dtype, dev, dh)
+    _vector("k_gain", k_gain, q.dtype, dev, dh)
+    n = 0 if inv_freq is None else inv_freq.numel()
+    _vector("inv_freq", inv_freq, torch.float32, dev, n)
+    _vector("positions", positions, torch.int32, dev, T)
+    return QkRotary(T, seq, nq, nk, dh, 2 * n, int(interleaved), eps, scale, lq, lk, lqo, lko)
+
+
+def op_qk_rotary_workspace_bytes(rows: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().dp_op_qk_rotary_workspace_bytes(rows, q_heads, kv_heads, head_dim))
+
+
+def op_qk_rotary_fwd(q, k, q_gain, k_gain, inv_freq, q_out, k_out, seq, interleaved=False, eps=1e-6, scale=1.0, positions=None,
+                     stream=None):
+    """Norm of every head (gains [head_dim], or None) and rotary position (inv_freq: fp32 [pairs turned], or None) of queries
+    q [rows, q_heads, head_dim] and keys k [rows, kv_heads, head_dim]; views of a packed projection will do."""
+    shape = _rotary_shape(q, k, q_out, k_out, q_gain, k_gain, inv_freq, positions, seq, interleaved, eps, scale)
+    _check(lib().dp_op_qk_rotary_fwd(_dt(q), C.byref(shape), _ptr(q), _ptr(k), _ptr(q_gain), _ptr(k_gain), _ptr(inv_freq),
+                                     _ptr(positions), _ptr(q_out), _ptr(k_out), _stream_ptr(stream)))
+
+
+def op_qk_rotary_bwd(dq_out, dk_out, q, k, q_gain, k_gain, inv_freq, dq, dk, dq_gain, dk_gain, ws, seq, interleaved=False, eps=1e-6,
+                     scale=1.0, positions=None, stream=None):
+    """The gradients of q, k (rows as dq, dk lie) and of the gains.  q and k may be None where there is no gain."""
+    shape = _rotary_shape(dq, dk, dq_out, dk_out, q_gain, k_gain, inv_freq, positions, seq, interleaved, eps, scale)
+    dev = dq.device
+    for name, x, of, ld, gain, dg in (("q", q, dq, shape.ldq_in, q_gain, dq_gain), ("k", k, dk, shape.ldk_in, k_gain, dk_gain)):
+        if x is not None and _heads(name, x, dq.dtype, dev, *of.shape) != ld:
+            _bad(f"{name} and its gradient must have the same row stride")
+        if gain is not None:
+            _vector(f"d{name}_gain", dg, dq.dtype, dev, of.shape[2], optional=False)
+    if (q_gain is not None or k_gain is not None) and (ws is None or ws.numel() * ws.element_size() <
+                                                       op_qk_rotary_workspace_bytes(*dq.shape[:2], dk.shape[1], dq.shape[2])):
+        _bad("the workspace is smaller than op_qk_rotary_workspace_bytes")
+    _check(lib().dp_op_qk_rotary_bwd(_dt(dq), C.byref(shape), _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(q_gain), _ptr(k_gain),
+                                     _ptr(inv_freq), _ptr(positions), _ptr(dq), _ptr(dk), _ptr(dq_gain), _ptr(dk_gain), _ptr(ws),
+                                     _stream_ptr(stream)))
 
 
 def probe_mfma(data, iters: int = 20000, stream=None):

@@ -179,6 +179,27 @@ hipError_t launch_attn_bwd_mfma_view(int B, int nh, int dh, int causal, const At
                                      const float *lse, const void *d_o, float *ws, hipStream_t s,
                                      const DropArgs *drop = nullptr);
 
+// ---- norms of queries and keys with rotary positions ---------------------------------------------
+// nq query and nk key heads of dh elements in rows of the given strides; forward q, k -> q_out, k_out, backward dq_out, dk_out
+// (rows as q_out, k_out) and q, k -> dq, dk (rows as q, k).  A gain of null: no norm.  half: pairs turned; positions null: row % seq.
+struct RotaryArgs {
+  int rows, seq, nq, nk, dh, half, interleaved;
+  float eps, scale;
+  long ldq_in, ldk_in, ldq_out, ldk_out;
+  const void *q, *k, *q_gain, *k_gain;
+  const float *freq;
+  const int32_t *positions;
+  void *q_out, *k_out;
+  const void *dq_out, *dk_out;
+  void *dq, *dk;
+  float *part;        // qk_rotary_ws_bytes, read only if there is a gain
+  int group, tokens;  // (the launchers' choice)
+};
+bool qk_rotary_supported(int dh);
+size_t qk_rotary_ws_bytes(int rows, int dh);
+hipError_t launch_qk_rotary_fwd(int dtype, RotaryArgs p, hipStream_t s);
+hipError_t launch_qk_rotary_bwd(int dtype, RotaryArgs p, void *dq_gain, void *dk_gain, hipStream_t s);
+
 // ---- diagnostics --------------------------------------------------------------
 // Matrix-core issue rate with operand fragments taken from `data` (bf16, n_elems >= 8); waits.
 hipError_t run_mfma_probe(const void *data, size_t n_elems, int iters, int n_cus, float *tflops, float *shader_mhz,

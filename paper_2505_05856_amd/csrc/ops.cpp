@@ -3,6 +3,7 @@
 #include "stage_internal.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 
@@ -284,6 +285,57 @@ dp_status dp_op_cross_attention_bwd(int32_t dtype, int32_t B, int32_t Sq, int32_
                                                  dropping ? &a : nullptr), "cross_attention_bwd");
 }
 
+
+// ---- norms of queries and keys with rotary positions
+static dp_status rotary_args(const char *what, int32_t dtype, const dp_qk_rotary *c, const float *inv_freq, dp::RotaryArgs *p) {
+  if (c == nullptr || bad_dtype(dtype)) return fail(DP_E_INVAL, "%s: bad argument", what);
+  if (c->rows < 0 || c->seq < 1 || c->q_heads < 0 || c->kv_heads < 0 || c->head_dim < 1 || (c->interleaved != 0 && c->interleaved != 1))
+    return fail(DP_E_INVAL, "%s: bad shape", what);
+  if (!dp::qk_rotary_supported(c->head_dim)) return fail(DP_E_UNSUPPORTED, "%s: head_dim must be even, <= 1024", what);
+  if (c->rot_dim < 0 || c->rot_dim > c->head_dim || c->rot_dim % 2) return fail(DP_E_INVAL, "%s: rot_dim must be even, 0..head_dim", what);
+  if (!(c->eps >= 0.f) || std::isinf(c->eps) || !std::isfinite(c->scale)) return fail(DP_E_INVAL, "%s: eps and scale must be finite, eps >= 0", what);
+  const int64_t wq = (int64_t)c->q_heads * c->head_dim, wk = (int64_t)c->kv_heads * c->head_dim;
+  if (c->ldq_in < wq || c->ldq_out < wq || c->ldk_in < wk || c->ldk_out < wk)
+    return fail(DP_E_INVAL, "%s: a row stride is shorter than the row's heads", what);
+  if (c->rows > 0 && c->rot_dim > 0 && c->q_heads + c->kv_heads > 0 && !inv_freq) return fail(DP_E_INVAL, "%s: inv_freq is null", what);
+  *p = dp::RotaryArgs{};
+  p->rows = c->rows; p->seq = c->seq; p->nq = c->q_heads; p->nk = c->kv_heads; p->dh = c->head_dim;
+  p->half = c->rot_dim / 2; p->interleaved = c->interleaved; p->eps = c->eps; p->scale = c->scale;
+  p->ldq_in = (long)c->ldq_in; p->ldk_in = (long)c->ldk_in; p->ldq_out = (long)c->ldq_out; p->ldk_out = (long)c->ldk_out;
+  p->freq = inv_freq;
+  return DP_OK;
+}
+
+size_t dp_op_qk_rotary_workspace_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+  if (rows < 0 || q_heads < 0 || kv_heads < 0 || head_dim < 0) return 0;
+  return dp::qk_rotary_ws_bytes(rows, head_dim);
+}
+
+dp_status dp_op_qk_rotary_fwd(int32_t dtype, const dp_qk_rotary *shape, const void *q, const void *k, const void *q_gain,
+                              const void *k_gain, const float *inv_freq, const int32_t *positions, void *q_out, void *k_out,
+                              void *hip_stream) {
+  dp::RotaryArgs p;
+  const dp_status st = rotary_args("qk_rotary_fwd", dtype, shape, inv_freq, &p);
+  if (st != DP_OK) return st;
+  if (p.rows > 0 && ((p.nq > 0 && (!q || !q_out)) || (p.nk > 0 && (!k || !k_out)))) return fail(DP_E_INVAL, "qk_rotary_fwd: null operand");
+  p.q = q; p.k = k; p.q_gain = q_gain; p.k_gain = k_gain; p.positions = positions; p.q_out = q_out; p.k_out = k_out;
+  return op_done(dp::launch_qk_rotary_fwd(dtype, p, (hipStream_t)hip_stream), "qk_rotary_fwd");
+}
+
+dp_status dp_op_qk_rotary_bwd(int32_t dtype, const dp_qk_rotary *shape, const void *dq_out, const void *dk_out, const void *q,
+                              const void *k, const void *q_gain, const void *k_gain, const float *inv_freq,
+                              const int32_t *positions, void *dq, void *dk, void *dq_gain, void *dk_gain, void *ws, void *hip_stream) {
+  dp::RotaryArgs p;
+  const dp_status st = rotary_args("qk_rotary_bwd", dtype, shape, inv_freq, &p);
+  if (st != DP_OK) return st;
+  if (p.rows > 0 && ((p.nq > 0 && (!dq_out || !dq || (q_gain && !q))) || (p.nk > 0 && (!dk_out || !dk || (k_gain && !k)))))
+    return fail(DP_E_INVAL, "qk_rotary_bwd: null operand");
+  if ((q_gain && !dq_gain) || (k_gain && !dk_gain) || ((q_gain || k_gain) && !ws))
+    return fail(DP_E_INVAL, "qk_rotary_bwd: a gain needs its gradient and a workspace");
+  p.q = q; p.k = k; p.q_gain = q_gain; p.k_gain = k_gain; p.positions = positions;
+  p.dq_out = dq_out; p.dk_out = dk_out; p.dq = dq; p.dk = dk; p.part = (float *)ws;
+  return op_done(dp::launch_qk_rotary_bwd(dtype, p, dq_gain, dk_gain, (hipStream_t)hip_stream), "qk_rotary_bwd");
+}
 
 dp_status dp_probe_mfma(const void *data_bf16, size_t n_elems, int32_t iters, float *tflops, float *shader_mhz,
                         void *hip_stream) {
