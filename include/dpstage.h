@@ -650,8 +650,8 @@ dp_status dp_op_cross_attention_bwd(int32_t dtype, int32_t B, int32_t Sq, int32_
  * (dtype, [head_dim], overwritten; not touched where the gain is NULL).  ws: device workspace of
  * dp_op_qk_rotary_workspace_bytes bytes, for gains' gradients only.
  * q_out may be q and dq may be dq_out (the same rows), k likewise; no other overlap.  head_dim is
- * even and at most 1024 (DP_E_UNSUPPORTED otherwise).  Any alignment: 16-byte accesses where
- * head_dim and rot_dim are multiples of 16, strides of 8 and pointers 16-byte aligned, element by
+ * even and at most 1024 (DP_E_UNSUPPORTED otherwise).  Any alignment: vector accesses where
+ * head_dim, rot_dim and the strides are multiples of 8 and pointers 16-byte aligned, element by
  * element otherwise.  No rows: nothing is read, gains' gradients become zero.  Heads of one kind
  * only: the other count 0, its pointers NULL. */
 typedef struct {
@@ -668,6 +668,38 @@ dp_status dp_op_qk_rotary_bwd(int32_t dtype, const dp_qk_rotary *shape, const vo
                               const void *k_gain /*nullable*/, const float *inv_freq,
                               const int32_t *positions /*nullable*/, void *dq, void *dk, void *dq_gain, void *dk_gain,
                               void *ws, void *hip_stream);
+
+/* Causal self-attention with a sliding window, first tokens that stay visible, shared key heads and
+ * padded samples.  Row b*seq + i of q is token i of sample b; it sees key j of its sample when
+ *   j <= i < len  and  (i - j < window  or  j < sinks),
+ * where len is lens[b] (int32 on the device, clamped to 0..seq) or, with lens NULL, seq; a window of
+ * seq or more is ordinary causal attention.  q has q_heads heads of head_dim, k and v kv_heads;
+ * query head h reads key head h / (q_heads / kv_heads).  Head h of a row is at column h*head_dim,
+ * rows lie ldq, ldk, ldv, ldo elements apart (column blocks of a packed projection will do).
+ *   o = softmax(scale * q k^T) v (rows as ldo), lse [batch, q_heads, seq] fp32 = log of the row sums
+ * A row past its sample's length sees nothing: o is 0 and lse -inf there, and its q, k, v are never
+ * read.  o or lse may be NULL.  The backward takes o, lse and d_o (rows as ldo) and writes dq, dk, dv
+ * (rows as q, k, v; dk and dv summed over the query heads that share the key head; rows past the
+ * length become 0); ws: device workspace of dp_op_window_attention_workspace_bytes bytes.  No
+ * overlap of an output with anything.  Sums and statistics fp32, results rounded once (in bf16 the
+ * probabilities and the logits' gradients are rounded to bf16 for the products they go into); the
+ * same bits at every call.  In bf16 a key or value that is not finite may spread to any row of its
+ * sample, not to other samples.  head_dim is a multiple of 8 and at most 256 (DP_E_UNSUPPORTED
+ * otherwise).  Any alignment; the matrix cores take head dimensions up to 128 with pointers 16-byte
+ * aligned, strides that are multiples of 16 bytes and samples that span less than 4 GiB, everything
+ * else goes to vector-ALU kernels 20 to 100 times slower. */
+typedef struct {
+  int32_t batch, seq, q_heads, kv_heads, head_dim, window, sinks;
+  float scale;
+  int64_t ldq, ldk, ldv, ldo;
+} dp_window_attention;
+size_t dp_op_window_attention_workspace_bytes(int32_t dtype, const dp_window_attention *shape);
+dp_status dp_op_window_attention_fwd(int32_t dtype, const dp_window_attention *shape, const void *q, const void *k,
+                                     const void *v, const int32_t *lens /*nullable*/, void *o, float *lse,
+                                     void *hip_stream);
+dp_status dp_op_window_attention_bwd(int32_t dtype, const dp_window_attention *shape, const void *q, const void *k,
+                                     const void *v, const int32_t *lens /*nullable*/, const void *o, const float *lse,
+                                     const void *d_o, void *dq, void *dk, void *dv, void *ws, void *hip_stream);
 
 /* Diagnostic for reading the roofline: the rate at which the matrix cores issue
  * v_mfma_f32_32x32x16_bf16 when nothing else limits them (operands in registers, 16

@@ -118,6 +118,12 @@ class QkRotary(C.Structure):
                [(n, C.c_int64) for n in ("ldq_in", "ldk_in", "ldq_out", "ldk_out")]
 
 
+class WindowAttention(C.Structure):
+    """dp_window_attention."""
+    _fields_ = [(n, C.c_int32) for n in ("batch", "seq", "q_heads", "kv_heads", "head_dim", "window", "sinks")] + \
+               [("scale", C.c_float)] + [(n, C.c_int64) for n in ("ldq", "ldk", "ldv", "ldo")]
+
+
 MEMOPT_VALIDATE = 1
 
 _lib = None
@@ -179,6 +185,10 @@ def lib() -> C.CDLL:
     L.dp_op_qk_rotary_workspace_bytes.argtypes = [i32, i32, i32, i32]
     L.dp_op_qk_rotary_fwd.argtypes = [i32, C.POINTER(QkRotary)] + [vp] * 9
     L.dp_op_qk_rotary_bwd.argtypes = [i32, C.POINTER(QkRotary)] + [vp] * 14
+    L.dp_op_window_attention_workspace_bytes.restype = sz
+    L.dp_op_window_attention_workspace_bytes.argtypes = [i32, C.POINTER(WindowAttention)]
+    L.dp_op_window_attention_fwd.argtypes = [i32, C.POINTER(WindowAttention)] + [vp] * 7
+    L.dp_op_window_attention_bwd.argtypes = [i32, C.POINTER(WindowAttention)] + [vp] * 12
     L.dp_partition.argtypes = [C.POINTER(StageConfig), C.POINTER(CostModel), i32, u64, u64, u64, C.POINTER(C.c_int64),
                                C.POINTER(u64), C.c_uint32, C.POINTER(i32), vp, sz, C.POINTER(PartitionStage),
                                C.POINTER(PartitionReport)]
@@ -192,7 +202,8 @@ def lib() -> C.CDLL:
                  "dp_op_gelu_fwd", "dp_op_gelu_bwd", "dp_op_gemm", "dp_op_gemm_tile", "dp_op_linear_bwd", "dp_op_linear_bwd_tiles", "dp_op_colsum", "dp_op_colsum_static", "dp_op_attention_fwd",
                  "dp_op_attention_bwd", "dp_op_dropout", "dp_op_attention_dropout_fwd", "dp_op_attention_dropout_bwd",
                  "dp_op_cross_attention_fwd", "dp_op_cross_attention_bwd",
-                 "dp_op_rmsnorm_fwd", "dp_op_rmsnorm_bwd", "dp_op_qk_rotary_fwd", "dp_op_qk_rotary_bwd"):
+                 "dp_op_rmsnorm_fwd", "dp_op_rmsnorm_bwd", "dp_op_qk_rotary_fwd", "dp_op_qk_rotary_bwd",
+                 "dp_op_window_attention_fwd", "dp_op_window_attention_bwd"):
         getattr(L, name).restype = i32
     _lib = L
     return L
@@ -644,12 +655,62 @@ def op_qk_rotary_bwd(dq_out, dk_out, q, k, q_gain, k_gain, inv_freq, dq, dk, dq_
             _bad(f"{name} and its gradient must have the same row stride")
         if gain is not None:
             _vector(f"d{name}_gain", dg, dq.dtype, dev, of.shape[2], optional=False)
-    if (q_gain is not None or k_gain is not None) and (ws is None or ws.numel() * ws.element_size() <
+    if (q_gain is not None or k_gain is not None) and (ws is None or ws.device != dev or ws.numel() * ws.element_size() <
                                                        op_qk_rotary_workspace_bytes(*dq.shape[:2], dk.shape[1], dq.shape[2])):
         _bad("the workspace is smaller than op_qk_rotary_workspace_bytes")
     _check(lib().dp_op_qk_rotary_bwd(_dt(dq), C.byref(shape), _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(q_gain), _ptr(k_gain),
                                      _ptr(inv_freq), _ptr(positions), _ptr(dq), _ptr(dk), _ptr(dq_gain), _ptr(dk_gain), _ptr(ws),
                                      _stream_ptr(stream)))
+
+
+def _window_shape(q, k, v, o, seq, window, sinks, scale, lens):
+    import torch
+    dev, (T, nq, dh) = _call_device(q), q.shape if q.dim() == 3 else (-1, -1, -1)
+    lq, lk = _heads("q", q, q.dtype, dev), _heads("k", k, q.dtype, dev, T, None, dh)
+    nk = k.shape[1]
+    lv = _heads("v", v, q.dtype, dev, T, nk, dh)
+    lo = nq * dh if o is None else _heads("o", o, q.dtype, dev, T, nq, dh)
+    if seq < 1 or T % seq:
+        _bad(f"{T} rows are no whole samples of {seq}")
+    _vector("lens", lens, torch.int32, dev, T // seq)
+    return WindowAttention(T // seq, seq, nq, nk, dh, window, sinks, dh ** -0.5 if scale is None else scale, lq, lk, lv, lo)
+
+
+def _row_sums(lse, q, seq):
+    import torch
+    _vector("lse", lse, torch.float32, q.device, q.shape[0] * q.shape[1])
+
+
+def op_window_attention_workspace_bytes(q, k, seq, window, sinks) -> int:
+    """For the backward of queries [rows, q_heads, head_dim] and keys [rows, kv_heads, head_dim]."""
+    T, nq, dh = q.shape
+    nk = k.shape[1]
+    return int(lib().dp_op_window_attention_workspace_bytes(
+        _dt(q), C.byref(WindowAttention(T // seq, seq, nq, nk, dh, window, sinks, 1.0, nq * dh, nk * dh, nk * dh, nq * dh))))
+
+
+def op_window_attention_fwd(q, k, v, seq, window, sinks, o, lse, lens=None, scale=None, stream=None):
+    """o, lse of causal attention over the `window` newest keys and the first `sinks` (scale: head_dim ** -0.5).  q and o are
+    [rows, q_heads, head_dim], k and v [rows, kv_heads, head_dim], rows in samples of `seq`; views of a packed projection will do."""
+    shape = _window_shape(q, k, v, o, seq, window, sinks, scale, lens)
+    _row_sums(lse, q, seq)
+    _check(lib().dp_op_window_attention_fwd(_dt(q), C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o), _ptr(lse),
+                                            _stream_ptr(stream)))
+
+
+def op_window_attention_bwd(q, k, v, o, lse, d_o, seq, window, sinks, dq, dk, dv, ws, lens=None, scale=None, stream=None):
+    """dq, dk, dv, which lie as q, k, v do (the same row strides); d_o as o."""
+    shape = _window_shape(q, k, v, o, seq, window, sinks, scale, lens)
+    _row_sums(lse, q, seq)
+    if lse is None or o is None:
+        _bad("the backward needs o and lse")
+    for name, t, of, ld in (("d_o", d_o, o, shape.ldo), ("dq", dq, q, shape.ldq), ("dk", dk, k, shape.ldk), ("dv", dv, v, shape.ldv)):
+        if _heads(name, t, q.dtype, q.device, *of.shape) != ld:
+            _bad(f"{name} must have the row stride of what it belongs to")
+    if ws is None or ws.device != q.device or ws.numel() * ws.element_size() < lib().dp_op_window_attention_workspace_bytes(_dt(q), C.byref(shape)):
+        _bad("the workspace is smaller than op_window_attention_workspace_bytes")
+    _check(lib().dp_op_window_attention_bwd(_dt(q), C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o), _ptr(lse), _ptr(d_o),
+                                            _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), _stream_ptr(stream)))
 
 
 def probe_mfma(data, iters: int = 20000, stream=None):

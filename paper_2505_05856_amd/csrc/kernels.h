@@ -179,6 +179,30 @@ hipError_t launch_attn_bwd_mfma_view(int B, int nh, int dh, int causal, const At
                                      const float *lse, const void *d_o, float *ws, hipStream_t s,
                                      const DropArgs *drop = nullptr);
 
+// ---- attention with a sliding window and first keys that stay visible -------------------------------
+// Query i of a sample sees key j when j <= i < len and (i - j < window or j < sinks).  Rows as in AttnView, with a stride each;
+// query head h reads key head h / (nq / nk).  lens null: every sample has S rows.  Backward: `ws` of window_ws_bytes.
+struct WindowArgs {
+  int B, S, nq, nk, dh, window, sinks;
+  float scale;
+  long ldq, ldk, ldv, ldo;
+  const void *q, *k, *v;
+  const int32_t *lens;
+  void *o;            // forward; nullable
+  float *lse;         // forward: written, nullable; backward: read
+  const void *o_in, *d_o;
+  void *dq, *dk, *dv;
+  float *ws;
+};
+// How many rows of sample b hold a sequence.
+__host__ __device__ inline int window_len(const WindowArgs &a, int n) { return a.lens == nullptr ? a.S : n < 0 ? 0 : n < a.S ? n : a.S; }
+size_t window_ws_bytes(int dtype, const WindowArgs &a);
+hipError_t launch_window_fwd(int dtype, const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_bwd(int dtype, const WindowArgs &a, hipStream_t s);
+// (any head dimension that is a multiple of 8 up to 256, any alignment: vector ALUs, a wavefront a row; ws: B * nq * S floats)
+hipError_t launch_window_fwd_simple(int dtype, const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_bwd_simple(int dtype, const WindowArgs &a, hipStream_t s);
+
 // ---- norms of queries and keys with rotary positions ---------------------------------------------
 // nq query and nk key heads of dh elements in rows of the given strides; forward q, k -> q_out, k_out, backward dq_out, dk_out
 // (rows as q_out, k_out) and q, k -> dq, dk (rows as q, k).  A gain of null: no norm.  half: pairs turned; positions null: row % seq.

@@ -337,6 +337,54 @@ dp_status dp_op_qk_rotary_bwd(int32_t dtype, const dp_qk_rotary *shape, const vo
   return op_done(dp::launch_qk_rotary_bwd(dtype, p, dq_gain, dk_gain, (hipStream_t)hip_stream), "qk_rotary_bwd");
 }
 
+// ---- attention with a sliding window
+static dp_status window_args(const char *what, int32_t dtype, const dp_window_attention *c, dp::WindowArgs *a) {
+  if (c == nullptr || bad_dtype(dtype)) return fail(DP_E_INVAL, "%s: bad argument", what);
+  if (c->batch < 0 || c->seq < 0 || c->q_heads < 1 || c->kv_heads < 1 || c->head_dim < 1 || c->q_heads % c->kv_heads)
+    return fail(DP_E_INVAL, "%s: bad shape (q_heads is a multiple of kv_heads)", what);
+  if (c->window < 1 || c->sinks < 0) return fail(DP_E_INVAL, "%s: window must be >= 1, sinks >= 0", what);
+  if (!(c->scale > 0.f) || !std::isfinite(c->scale)) return fail(DP_E_INVAL, "%s: scale must be positive and finite", what);
+  if (c->head_dim % 8 || c->head_dim > 256) return fail(DP_E_UNSUPPORTED, "%s: head_dim must be a multiple of 8, <= 256", what);
+  const int64_t wq = (int64_t)c->q_heads * c->head_dim, wk = (int64_t)c->kv_heads * c->head_dim;
+  if (c->ldq < wq || c->ldo < wq || c->ldk < wk || c->ldv < wk) return fail(DP_E_INVAL, "%s: a row stride is shorter than the row's heads", what);
+  if ((int64_t)c->batch * c->seq > INT32_MAX || (int64_t)c->batch * c->q_heads > INT32_MAX / 64)
+    return fail(DP_E_UNSUPPORTED, "%s: more than 2^31 rows", what);
+  *a = dp::WindowArgs{};
+  a->B = c->batch; a->S = c->seq; a->nq = c->q_heads; a->nk = c->kv_heads; a->dh = c->head_dim;
+  a->window = c->window; a->sinks = c->sinks; a->scale = c->scale;
+  a->ldq = (long)c->ldq; a->ldk = (long)c->ldk; a->ldv = (long)c->ldv; a->ldo = (long)c->ldo;
+  return DP_OK;
+}
+
+size_t dp_op_window_attention_workspace_bytes(int32_t dtype, const dp_window_attention *shape) {
+  dp::WindowArgs a;
+  return window_args("window_attention", dtype, shape, &a) == DP_OK ? dp::window_ws_bytes(dtype, a) : 0;
+}
+
+dp_status dp_op_window_attention_fwd(int32_t dtype, const dp_window_attention *shape, const void *q, const void *k, const void *v,
+                                     const int32_t *lens, void *o, float *lse, void *hip_stream) {
+  dp::WindowArgs a;
+  const dp_status st = window_args("window_attention_fwd", dtype, shape, &a);
+  if (st != DP_OK) return st;
+  if ((long)a.B * a.S == 0 || (!o && !lse)) return DP_OK;
+  if (!q || !k || !v) return fail(DP_E_INVAL, "window_attention_fwd: null operand");
+  a.q = q; a.k = k; a.v = v; a.lens = lens; a.o = o; a.lse = lse;
+  return op_done(dp::launch_window_fwd(dtype, a, (hipStream_t)hip_stream), "window_attention_fwd");
+}
+
+dp_status dp_op_window_attention_bwd(int32_t dtype, const dp_window_attention *shape, const void *q, const void *k, const void *v,
+                                     const int32_t *lens, const void *o, const float *lse, const void *d_o, void *dq, void *dk,
+                                     void *dv, void *ws, void *hip_stream) {
+  dp::WindowArgs a;
+  const dp_status st = window_args("window_attention_bwd", dtype, shape, &a);
+  if (st != DP_OK) return st;
+  if ((long)a.B * a.S == 0) return DP_OK;
+  if (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv || !ws) return fail(DP_E_INVAL, "window_attention_bwd: null operand");
+  a.q = q; a.k = k; a.v = v; a.lens = lens; a.o_in = o; a.lse = const_cast<float *>(lse); a.d_o = d_o;
+  a.dq = dq; a.dk = dk; a.dv = dv; a.ws = (float *)ws;
+  return op_done(dp::launch_window_bwd(dtype, a, (hipStream_t)hip_stream), "window_attention_bwd");
+}
+
 dp_status dp_probe_mfma(const void *data_bf16, size_t n_elems, int32_t iters, float *tflops, float *shader_mhz,
                         void *hip_stream) {
   if (!data_bf16 || n_elems < 8 || n_elems % 8 || iters < 1 || !tflops || !shader_mhz)
