@@ -202,6 +202,11 @@ hipError_t launch_window_bwd(int dtype, const WindowArgs &a, hipStream_t s);
 // (any head dimension that is a multiple of 8 up to 256, any alignment: vector ALUs, a wavefront a row; ws: B * nq * S floats)
 hipError_t launch_window_fwd_simple(int dtype, const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_bwd_simple(int dtype, const WindowArgs &a, hipStream_t s);
+// (bf16 on the matrix cores; window and sinks at most S)
+bool window_mfma_supported(const WindowArgs &a);
+size_t window_mfma_ws_bytes(const WindowArgs &a);
+hipError_t launch_window_fwd_mfma(const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_bwd_mfma(const WindowArgs &a, hipStream_t s);
 
 // ---- norms of queries and keys with rotary positions ---------------------------------------------
 // nq query and nk key heads of dh elements in rows of the given strides; forward q, k -> q_out, k_out, backward dq_out, dk_out

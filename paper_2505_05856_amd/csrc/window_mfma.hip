@@ -1,0 +1,815 @@
+// Sliding-window attention on the matrix cores (bf16 in, fp32 accumulate): query i of a sample sees key j when j <= i < len and
+// (i - j < window or j < sinks).  The tiles, layouts and pipelines are those of the full attention; what is different:
+//
+// - A block of 128 queries walks two runs of 64-key tiles, those that hold the first keys and those of its window, as one list:
+//   the loads of the second run's start are in flight while the first run ends.
+// - Which keys of a tile a lane's query sees is a 32-bit word (three shifts), from which each logit takes a bit: two
+//   instructions a logit, as a causal mask alone would take, and only in tiles that hold hidden keys.
+// - Query heads that share a key head are separate blocks forward and for dQ (next to each other, so one L2 serves their keys);
+//   dK and dV walk the queries of all of them, tile after tile, so no gradient is added up outside a block ...
+// - ... unless that leaves CUs idle, or keys are seen by every later query (the first ones): such a walk is cut into parts of
+//   about the length of the others; each leaves fp32 sums in the workspace, and a last kernel adds them in a fixed order.
+// - Rows past a sample's length are never read (tiles end with copies of the last row, whose products are masked) and become 0.
+// - Head dimensions of 8..128: kernels for 64 and 128 columns; columns past the head are zeros on the side that waits in
+//   registers and copies of the first ones in LDS, and are not stored.
+#include "attn_tile.h"
+
+#include <type_traits>
+
+namespace dp {
+
+namespace {
+
+// ---- what a query, or a key, sees ------------------------------------------------------------------
+// bits x and up of a 32-bit word (any x)
+__device__ __forceinline__ uint32_t bits_from(int x) { return (uint32_t)(0xffffffffull << min(max(x, 0), 32)); }
+// the hidden ones of keys jb .. jb+31 for query i
+__device__ __forceinline__ uint32_t hidden_keys(int i, int jb, int window, int sinks) {
+  return bits_from(i + 1 - jb) | (bits_from(sinks - jb) & ~bits_from(i - window + 1 - jb));
+}
+// the hidden ones of queries ib .. ib+31 for key j
+__device__ __forceinline__ uint32_t hidden_queries(int j, int ib, int window, int sinks) {
+  return ~bits_from(j - ib) | (j < sinks ? 0u : bits_from(j + window - ib));
+}
+// -inf for the hidden ones of a 32x32 result's 16 elements a lane (rows acc_row(e, lane))
+__device__ __forceinline__ void hide(f32x16 &v, uint32_t hidden, int hh) {
+  const int h = (int)(hidden >> (4 * hh));
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int m = __builtin_amdgcn_sbfe(h, 8 * (e >> 2) + (e & 3), 1);   // all ones where hidden
+    v[e] = __int_as_float((m & 0xff800000) | (~m & __float_as_int(v[e])));
+  }
+}
+
+// The key tiles (64 keys) that a block of queries q0 .. q0+127 walks: the first `head` tiles, then tiles from `from` on.
+struct KeyTiles {
+  int head, gap, n;   // n: how many in all; tile t of the walk is t, or t + gap from `head` on
+  __device__ __forceinline__ KeyTiles(int q0, int len, int window, int sinks) {
+    const int end = (min(q0 + BROWS, len) - 1) / BKV + 1, w0 = max(q0 - window + 1, 0) / BKV;
+    head = min((sinks + BKV - 1) / BKV, w0);
+    gap = w0 - head;
+    n = end - gap;
+  }
+  __device__ __forceinline__ int first_key(int t) const { return (t < head ? t : t + gap) * BKV; }
+};
+
+// Rows of sample b that hold a sequence (the same in every lane, and known to be)
+__device__ __forceinline__ int sample_len(const WindowArgs &a, int b) {
+  return __builtin_amdgcn_readfirstlane(window_len(a, a.lens != nullptr ? a.lens[b] : 0));
+}
+
+// ---- tiles whose heads may be narrower than the kernel ---------------------------------------------------
+// request i of the DH/32 a wave issues for a tile (as dma_req_both): chunks past the head's `nch` read its first
+template <int DH>
+__device__ __forceinline__ void dma_req(int i, unsigned lds_byte, const char *src, unsigned ldb, int row0, int nrows, int nch, int wave,
+                                        int lane) {
+  constexpr int NREQ = DH / 32, RPR = 1024 / (DH * 2), CPR = DH / 8;
+  const int q = wave * NREQ + i, r = RPR * q + lane / CPR;
+  const int rg = min(row0 + r, nrows - 1);
+  const int chunk = (int)((unsigned)(lane % CPR) ^ swz_both<DH>((unsigned)r));
+  dma16(lds_byte + (unsigned)q * 1024u, (unsigned)rg * ldb + (unsigned)(chunk < nch ? chunk : 0) * 16u, src);
+}
+template <int DH>
+__device__ __forceinline__ void dma_tile(unsigned lds_byte, const char *src, unsigned ldb, int row0, int nrows, int nch, int wave, int lane) {
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i) dma_req<DH>(i, lds_byte, src, ldb, row0, nrows, nch, wave, lane);
+}
+// elements 16 kd + 8 (lane / 32) .. of a row as an operand fragment, zeros past the head
+__device__ __forceinline__ bf16x8 row_frag(const bf16 *row, int kd, int hh, int dh) {
+  const int at = kd * 16 + 8 * hh;
+  const uint4 v = ld16(row + (at < dh ? at : 0));   // (unguarded: the compiler would wait for each load on its own)
+  return as_frag(at < dh ? v : make_uint4(0u, 0u, 0u, 0u));
+}
+// as store_rows_via_lds, for heads of `nch` 16-byte chunks; rows from `valid` on become zeros
+template <int DH>
+__device__ __forceinline__ void store_rows(unsigned char *ew, const f32x16 (&acc)[DH / 32], float mul, bf16 *dst, long ld, int nrows,
+                                           int valid, int nch, int lane) {
+  constexpr int ND = DH / 32, CPR = DH / 8, RPI = 64 / CPR;
+  const int row = lane & 31, hh = lane >> 5;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      bf16x4 v;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[t] = (bf16)(acc[d][e4 * 4 + t] * mul);
+      const int pos = (d * 4 + e4) ^ (row & (CPR - 1));
+      *reinterpret_cast<bf16x4 *>(ew + row * (DH * 2) + pos * 16 + hh * 8) = v;
+    }
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; ++i) {
+    const int r = i * RPI + lane / CPR, c = lane % CPR;
+    uint4 q = *reinterpret_cast<const uint4 *>(ew + r * (DH * 2) + ((c ^ (r & (CPR - 1))) * 16));
+    if (r >= valid) q = make_uint4(0u, 0u, 0u, 0u);
+    if (r < nrows && c < nch) *reinterpret_cast<uint4 *>(dst + (long)r * ld + c * 8) = q;
+  }
+}
+// rows r0 .. r1-1 of a head become zeros (by the whole block)
+__device__ __forceinline__ void zero_rows(bf16 *dst, long ld, int r0, int r1, int nch) {
+  for (int i = threadIdx.x; i < (r1 - r0) * nch; i += 256) {
+    const int r = r0 + i / nch, c = i % nch;
+    *reinterpret_cast<uint4 *>(dst + (long)r * ld + c * 8) = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// ------------------------------------------------------------------ forward
+// The pipeline of a tile is the full attention's (attn_mfma.hip): the logits of tile t+1 are taken beside the softmax of tile t.
+template <int DH, bool ORDERED>
+__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void window_fwd_kernel(WindowArgs a, RowOrder ro) {
+  constexpr int ND = DH / 32, NK = DH / 16;
+  // LDS, in bytes: [K even][K odd][V even][V odd]; tile t of the walk lives in the buffers of t's parity
+  constexpr unsigned TILE = BKV * DH * 2, VOFF = 2 * TILE;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
+
+  const int S = a.S, nqt = (S + BROWS - 1) / BROWS, nch = a.dh / 8;
+  int rank, head;
+  row_tile<ORDERED>(ro, blockIdx.x, gridDim.x, nqt, &rank, &head);
+  const int q0 = (nqt - 1 - rank) * BROWS;   // (late tiles are the heavy ones)
+  const int h = head % a.nq, b = head / a.nq, kh = h / (a.nq / a.nk);
+  const int len = sample_len(a, b);
+  const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int iw0 = q0 + wave * 32, qi = iw0 + (lane & 31);
+  bf16 *ob = (bf16 *)a.o + (long)b * S * a.ldo + (long)h * a.dh;
+  float *lb = a.lse + ((long)b * a.nq + h) * S;
+  if (q0 >= len) {
+    const int r1 = min(q0 + BROWS, S);
+    if (a.o != nullptr) zero_rows(ob, a.ldo, q0, r1, nch);
+    if (a.lse != nullptr && q0 + tid < r1) lb[q0 + tid] = -INFINITY;
+    return;
+  }
+  const bf16 *qb = (const bf16 *)a.q + (long)b * S * a.ldq + (long)h * a.dh;
+  const char *kb = uniform_ptr((const char *)((const bf16 *)a.k + (long)b * S * a.ldk + (long)kh * a.dh));
+  const char *vb = uniform_ptr((const char *)((const bf16 *)a.v + (long)b * S * a.ldv + (long)kh * a.dh));
+  const unsigned ldkb = (unsigned)a.ldk * 2u, ldvb = (unsigned)a.ldv * 2u;
+  const float c = a.scale * kLog2e;
+  const int window = a.window, sinks = a.sinks;
+  const KeyTiles kt(q0, len, window, sinks);
+  // whether tile t of the walk hides a key from a query of the block
+  auto hides = [&](int t) {
+    const int j0 = kt.first_key(t);
+    return j0 + BKV - 1 > q0 || (q0 + BROWS - 1 - j0 >= window && j0 + BKV > sinks);
+  };
+
+  auto fetch_k = [&](int t) { dma_tile<DH>((unsigned)(t & 1) * TILE, kb, ldkb, kt.first_key(t), len, nch, wave, lane); };
+  fetch_k(0);
+  dma_tile<DH>(VOFF, vb, ldvb, kt.first_key(0), len, nch, wave, lane);
+  if (kt.n > 1) fetch_k(1);
+
+  bf16x8 qf[NK];
+  const bf16 *qrow = qb + (long)min(qi, len - 1) * a.ldq;   // (a query past the end reads the last row, and nothing of it is stored)
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd) qf[kd] = row_frag(qrow, kd, hh, a.dh);
+
+  f32x16 acc[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
+  float m = -1e30f, l = 0.f;   // m: reference point of the exponents (log2 domain)
+
+  BothAddr<DH> at;
+  at.init(lane);
+  wait_dma();
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd) asm volatile("" ::"v"(qf[kd]));   // (the fragments are waited for here, not in the tile loop)
+  __syncthreads();
+
+  bf16x8 fx[2];                  // fragment double buffer
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  auto ld_k = [&](unsigned buf, int slot, int sub, int kd) { fx[slot] = at.rows(buf, sub * 32, kd); };
+  auto ld_v = [&](unsigned buf, int slot, int sub, int j) { fx[slot] = at.cols(buf, sub * 32 + (j / ND) * 16, j % ND); };
+  auto zero = [](f32x16 &v) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = 0.f;
+  };
+  auto mask = [&](f32x16 (&sv)[2], int j0) {
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) hide(sv[sub], hidden_keys(qi, j0 + 32 * sub, window, sinks), hh);
+  };
+  f32x16 lg[2][2];         // raw logits: those of tile t in lg[t & 1]
+  float mx = -INFINITY;    // maximum over the raw logits of the tile about to be worked on (this lane's keys)
+
+  auto tile = [&](int t, auto par_tag, auto more_tag) {
+    constexpr int PAR = decltype(par_tag)::value;
+    constexpr bool MORE = decltype(more_tag)::value;
+    constexpr unsigned KN = (PAR ^ 1) * TILE, V = VOFF + PAR * TILE;   // K of tile t+1, V of tile t
+    f32x16 (&cur)[2] = lg[PAR], (&nxt)[2] = lg[PAR ^ 1];
+    mx = halves_max(mx);
+    const float m_new = fmaxf(m, mx * c);
+    constexpr float kLag = 8.f;   // (the reference point follows the maximum only when it is left behind by a factor of 2^8)
+    if (__builtin_amdgcn_ballot_w64(m_new > m + kLag) != 0) {
+      const float alpha = fast_exp2(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+      m = m_new;
+    }
+    mx = -INFINITY;
+    float ps = 0.f;
+    auto soft = [&](f32x16 &sv, int e0, int n) {
+#pragma unroll
+      for (int u = 0; u < n; ++u) {
+        sv[e0 + u] = fast_exp2(__builtin_fmaf(sv[e0 + u], c, -m));
+        ps += sv[e0 + u];
+      }
+    };
+    auto vmax = [&](const f32x16 &sv, int e0, int n) {
+#pragma unroll
+      for (int u = 0; u < n; ++u) mx = fmaxf(mx, sv[e0 + u]);
+    };
+    const int jn = kt.first_key(t + 1), jnn = kt.first_key(t + 2);
+    if (MORE) { zero(nxt[0]); zero(nxt[1]); ld_k(KN, 0, 0, 0); ld_k(KN, 1, 1, 0); }
+#pragma unroll
+    for (int kd = 0; kd < NK; ++kd) {
+      if (MORE) {
+        // (past the walk's end the requests read rows it has, and nobody reads them)
+        if (kd < NK / 2) dma_req<DH>(kd, PAR * TILE, kb, ldkb, jnn, len, nch, wave, lane);
+        else dma_req<DH>(kd - NK / 2, VOFF + (PAR ^ 1) * TILE, vb, ldvb, jn, len, nch, wave, lane);
+        const bf16x8 ka = fx[0], kb2 = fx[1];
+        if (kd + 1 < NK) { ld_k(KN, 0, 0, kd + 1); ld_k(KN, 1, 1, kd + 1); }
+        nxt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[kd], nxt[0], 0, 0, 0);
+        nxt[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb2, qf[kd], nxt[1], 0, 0, 0);
+      }
+      if (kd + 1 == NK) ld_v(V, 0, 0, 0);
+      soft(cur[0], kd * (16 / NK), 16 / NK);
+      fence();
+    }
+    if (MORE && hides(t + 1)) mask(nxt, jn);
+    bf16x8 pf[2];
+    pf[0] = pack8(cur[0], 0); pf[1] = pack8(cur[0], 8);
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      if (j + 1 < NK) ld_v(V, (j + 1) & 1, 0, j + 1); else ld_v(V, (j + 1) & 1, 1, 0);
+      acc[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], pf[j / ND], acc[j % ND], 0, 0, 0);
+      if ((j * 8) % NK == 0) soft(cur[1], j * 8 / NK, 8 / NK >= 1 ? 8 / NK : 1);
+      if (MORE) vmax(nxt[0], j * (16 / NK), 16 / NK);
+      fence();
+    }
+    pf[0] = pack8(cur[1], 0);
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {
+      if (j + 1 < NK) ld_v(V, (j + 1) & 1, 1, j + 1);
+      if (j == ND) pf[1] = pack8(cur[1], 8);
+      acc[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], pf[j / ND], acc[j % ND], 0, 0, 0);
+      if (j < ND) soft(cur[1], 8 + j * (8 / ND), 8 / ND);
+      else if (MORE) vmax(nxt[1], (j - ND) * (16 / ND), 16 / ND);
+      fence();
+    }
+    l += ps;
+    wait_dma();        // this wave's parts of the tiles on their way are in
+    __syncthreads();   // everyone's are, and everyone is done with this tile's
+  };
+
+  using P0 = std::integral_constant<int, 0>;
+  using P1 = std::integral_constant<int, 1>;
+  using Yes = std::true_type;
+  using No = std::false_type;
+  zero(lg[0][0]); zero(lg[0][1]);
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd) {
+    lg[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.rows(0u, 0, kd), qf[kd], lg[0][0], 0, 0, 0);
+    lg[0][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(at.rows(0u, 32, kd), qf[kd], lg[0][1], 0, 0, 0);
+  }
+  if (hides(0)) mask(lg[0], kt.first_key(0));
+#pragma unroll
+  for (int e = 0; e < 16; ++e) mx = fmaxf(mx, fmaxf(lg[0][0][e], lg[0][1][e]));
+  __syncthreads();   // everyone has read K tile 0: the first tile below refills its buffer with K tile 2
+  int t = 0;
+  for (; t + 2 < kt.n; t += 2) {
+    tile(t, P0{}, Yes{});
+    tile(t + 1, P1{}, Yes{});
+  }
+  if (t + 1 < kt.n) {   // (the last tile has one form, that of even t: an odd one is made to look even)
+    tile(t, P0{}, Yes{});
+    lg[0][0] = lg[1][0]; lg[0][1] = lg[1][1];
+    at.flip_cols(TILE);
+    ++t;
+  }
+  tile(t, P0{}, No{});
+
+  l += __shfl_xor(l, 32, 64);
+  if (a.lse != nullptr && hh == 0 && qi < S) lb[qi] = qi < len ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  if (a.o == nullptr) return;
+  store_rows<DH>(smem_b + wave * (64 * DH), acc, 1.0f / l, ob + (long)iw0 * a.ldo, a.ldo, S - iw0, len - iw0, nch, lane);
+}
+
+// ------------------------------------------------------------------ backward: dQ, and the row dots <dO_i, O_i>
+template <int DH, bool ORDERED>
+__global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrder ro) {
+  constexpr int ND = DH / 32, NK = DH / 16;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
+  constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE;   // [stage 0: K, V][stage 1: K, V]
+
+  const int S = a.S, nqt = (S + BROWS - 1) / BROWS, nch = a.dh / 8;
+  int rank, head;
+  row_tile<ORDERED>(ro, blockIdx.x, gridDim.x, nqt, &rank, &head);
+  const int q0 = (nqt - 1 - rank) * BROWS;
+  const int h = head % a.nq, b = head / a.nq, kh = h / (a.nq / a.nk);
+  const int len = sample_len(a, b);
+  const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  bf16 *dqb = (bf16 *)a.dq + (long)b * S * a.ldq + (long)h * a.dh;
+  if (q0 >= len) {
+    zero_rows(dqb, a.ldq, q0, min(q0 + BROWS, S), nch);
+    return;
+  }
+  const bf16 *qb = (const bf16 *)a.q + (long)b * S * a.ldq + (long)h * a.dh;
+  const char *ksrc = uniform_ptr((const char *)((const bf16 *)a.k + (long)b * S * a.ldk + (long)kh * a.dh));
+  const char *vsrc = uniform_ptr((const char *)((const bf16 *)a.v + (long)b * S * a.ldv + (long)kh * a.dh));
+  const unsigned ldkb = (unsigned)a.ldk * 2u, ldvb = (unsigned)a.ldv * 2u;
+  const int iw0 = q0 + wave * 32, qi = iw0 + (lane & 31);
+  const float c = a.scale * kLog2e;
+  const int window = a.window, sinks = a.sinks;
+  const KeyTiles kt(q0, len, window, sinks);
+  auto fetch = [&](int t, unsigned buf) {
+    const int j0 = kt.first_key(t);
+    dma_tile<DH>(buf, ksrc, ldkb, j0, len, nch, wave, lane);
+    dma_tile<DH>(buf + TILE, vsrc, ldvb, j0, len, nch, wave, lane);
+  };
+  fetch(0, 0u);
+
+  const long qc = min(qi, len - 1);
+  const bf16 *qrow = qb + qc * a.ldq;
+  const bf16 *grow = (const bf16 *)a.d_o + (long)b * S * a.ldo + (long)h * a.dh + qc * a.ldo;
+  const bf16 *orow = (const bf16 *)a.o_in + (long)b * S * a.ldo + (long)h * a.dh + qc * a.ldo;
+  bf16x8 qf[NK], gf[NK], of[NK];
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd) {
+    qf[kd] = row_frag(qrow, kd, hh, a.dh);
+    gf[kd] = row_frag(grow, kd, hh, a.dh);
+    of[kd] = row_frag(orow, kd, hh, a.dh);
+  }
+  float dsum = 0.f;
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dsum += (float)of[kd][i] * (float)gf[kd][i];
+  const float dq_i = dsum + __shfl_xor(dsum, 32, 64);   // the two halves of the row
+  const long row_at = ((long)b * a.nq + h) * S + qi;
+  if (qi < len && hh == 0) a.ws[row_at] = dq_i;
+  const float lq = qi < len ? a.lse[row_at] * kLog2e : INFINITY;   // (queries past the end: P = 0)
+
+  f32x16 dq[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dq[d][e] = 0.f;
+
+  BothAddr<DH> at;
+  at.init(lane);
+  wait_dma();
+  __syncthreads();
+
+  // the pipeline over the two 32-key sub-tiles A and B of a tile, as in the full attention's dQ kernel
+  constexpr int EPS = 16 / NK;
+  bf16x8 fx[2], fy[2];
+  auto ld_rows = [&](int slot, int sub, int kd) {   // K and V along the rows: operands of S and dP
+    fx[slot] = at.rows(0u, sub * 32, kd);
+    fy[slot] = at.rows(TILE, sub * 32, kd);
+  };
+  auto ld_cols = [&](int slot, int sub, int j) {    // K down the rows: operand of dQ
+    fx[slot] = at.cols(0u, sub * 32 + (j / ND) * 16, j % ND);
+  };
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  f32x16 sA, dpA;
+  auto logits_of_a = [&] {
+    ld_rows(0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { sA[e] = 0.f; dpA[e] = 0.f; }
+#pragma unroll
+    for (int kd = 0; kd < NK; ++kd) {
+      if (kd + 1 < NK) ld_rows((kd + 1) & 1, 0, kd + 1); else ld_rows((kd + 1) & 1, 1, 0);
+      sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], qf[kd], sA, 0, 0, 0);
+      dpA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], gf[kd], dpA, 0, 0, 0);
+      fence();
+    }
+  };
+  logits_of_a();
+
+  for (int t = 0; t < kt.n; ++t) {
+    const int j0 = kt.first_key(t);
+    if (t + 1 < kt.n) fetch(t + 1, (unsigned)((t & 1) ^ 1) * STAGE);   // (every wave left that stage at the barrier below)
+    {
+      auto mask = [&](f32x16 &sv, int sub) {
+        const int jb = j0 + 32 * sub;
+        if (jb + 31 > iw0 || (iw0 + 31 - jb >= window && jb + 32 > sinks)) hide(sv, hidden_keys(qi, jb, window, sinks), hh);
+      };
+      auto soft = [&](f32x16 &sv, f32x16 &dpv, int e0) {   // logits -> P, dP -> dS
+#pragma unroll
+        for (int u = 0; u < EPS; ++u) {
+          const int e = e0 + u;
+          dpv[e] = fast_exp2(sv[e] * c - lq) * (dpv[e] - dq_i);
+        }
+      };
+      f32x16 sB, dpB;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { sB[e] = 0.f; dpB[e] = 0.f; }
+      mask(sA, 0);
+#pragma unroll
+      for (int kd = 0; kd < NK; ++kd) {   // stage 1
+        if (kd + 1 < NK) ld_rows((kd + 1) & 1, 1, kd + 1); else ld_cols((kd + 1) & 1, 0, 0);
+        sB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], qf[kd], sB, 0, 0, 0);
+        dpB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], gf[kd], dpB, 0, 0, 0);
+        soft(sA, dpA, kd * EPS);
+        fence();
+      }
+      bf16x8 dsf[2];
+      dsf[0] = pack8(dpA, 0); dsf[1] = pack8(dpA, 8);
+      mask(sB, 1);
+#pragma unroll
+      for (int j = 0; j < NK; ++j) {      // stage 2
+        if (j + 1 < NK) ld_cols((j + 1) & 1, 0, j + 1); else ld_cols((j + 1) & 1, 1, 0);
+        dq[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], dsf[j / ND], dq[j % ND], 0, 0, 0);
+        soft(sB, dpB, j * EPS);
+        fence();
+      }
+      dsf[0] = pack8(dpB, 0); dsf[1] = pack8(dpB, 8);
+#pragma unroll
+      for (int j = 0; j < NK; ++j) {      // stage 3
+        if (j + 1 < NK) ld_cols((j + 1) & 1, 1, j + 1);
+        dq[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], dsf[j / ND], dq[j % ND], 0, 0, 0);
+        fence();
+      }
+    }
+    at.flip(STAGE);
+    wait_dma();
+    __syncthreads();
+    if (t + 1 < kt.n) logits_of_a();   // stage 4
+  }
+
+  store_rows<DH>(smem_b + wave * (64 * DH), dq, a.scale, dqb + (long)iw0 * a.ldq, a.ldq, S - iw0, len - iw0, nch, lane);
+}
+
+// ------------------------------------------------------------------ backward: dK and dV
+// How the walks over query tiles (64 queries) are cut.  Key block kb (128 keys) of a key head walks, for each query head of its
+// group, the tiles from its own first to the end of its window: `parts` pieces.  Key blocks below `first` hold keys that all
+// later queries see: the rest of the sequence, `far` pieces more.
+struct KeyWork { int key_blocks, parts, first, far; };
+
+struct Walk { int t0, nt, begin, end; };   // query tiles t0 .. t0+nt-1 of each head in turn; items begin .. end-1 of that list
+__host__ __device__ __forceinline__ Walk walk_of(const KeyWork &w, int kb, int piece, int len, int window, int group) {
+  const int tiles = (len + BKV - 1) / BKV, t0 = 2 * kb;
+  const long last = ((long)kb * BROWS + BROWS - 1 + window - 1) / BKV;   // the last tile of the window
+  const int t1 = last + 1 < tiles ? (int)last + 1 : tiles;
+  Walk r;
+  const bool far = piece >= w.parts;
+  r.t0 = far ? (t1 > t0 ? t1 : t0) : t0;
+  const int end = far ? tiles : t1;
+  r.nt = end > r.t0 ? end - r.t0 : 0;
+  const int n = r.nt * group, pieces = far ? w.far : w.parts, chunk = (n + pieces - 1) / pieces, i = far ? piece - w.parts : piece;
+  r.begin = i * chunk < n ? i * chunk : n;
+  r.end = r.begin + chunk < n ? r.begin + chunk : n;
+  return r;
+}
+// Where a piece's sums go: a slot of the workspace (two [128][DH] arrays), or -1: it is its block's only one, the result itself.
+__host__ __device__ __forceinline__ long slot_of(const KeyWork &w, long head, int kb, int piece) {
+  const int sinks_at = w.key_blocks * w.parts;   // slots a head: those of the windows, where they have several, then the far ones
+  if (w.parts == 1) return kb >= w.first ? -1 : head * (long)w.first * (1 + w.far) + (long)kb * (1 + w.far) + piece;
+  return head * ((long)sinks_at + (long)w.first * w.far) +
+         (piece < w.parts ? (long)kb * w.parts + piece : sinks_at + (long)kb * w.far + piece - w.parts);
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
+                                                                          float *__restrict__ sums) {
+  constexpr int ND = DH / 32, NK = DH / 16;
+  // LDS, in bytes: [stage 0: Q, dO][stage 1: Q, dO][stage 0: lse, row dots][stage 1: lse, row dots]
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
+  constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE, FBASE = 2 * STAGE, FSTAGE = 8 * BKV;
+
+  const int S = a.S, nch = a.dh / 8, group = a.nq / a.nk;
+  // a head's pieces: the far ones first, then the windows' from the first key block on
+  const int per_head = w.key_blocks * w.parts + w.first * w.far;
+  const int wid = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int head = wid / per_head, id = wid - head * per_head, nfar = w.first * w.far;
+  const int kb = id < nfar ? id / w.far : (id - nfar) / w.parts;
+  const int piece = id < nfar ? w.parts + id % w.far : (id - nfar) % w.parts;
+  const int kh = head % a.nk, b = head / a.nk;
+  const int len = sample_len(a, b);
+  const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j0 = kb * BROWS, jw0 = j0 + wave * 32, kj = jw0 + (lane & 31);
+  const long slot = slot_of(w, head, kb, piece);
+  bf16 *dkb = (bf16 *)a.dk + (long)b * S * a.ldk + (long)kh * a.dh, *dvb = (bf16 *)a.dv + (long)b * S * a.ldv + (long)kh * a.dh;
+  if (j0 >= len) {
+    if (slot < 0) {
+      zero_rows(dkb, a.ldk, j0, min(j0 + BROWS, S), nch);
+      zero_rows(dvb, a.ldv, j0, min(j0 + BROWS, S), nch);
+    }
+    return;
+  }
+  const Walk walk = walk_of(w, kb, piece, len, a.window, group);
+  if (slot >= 0 && walk.begin == walk.end) return;   // (the kernel that adds the pieces up knows)
+  const bf16 *krow = (const bf16 *)a.k + ((long)b * S + min(kj, len - 1)) * a.ldk + (long)kh * a.dh;
+  const bf16 *vrow = (const bf16 *)a.v + ((long)b * S + min(kj, len - 1)) * a.ldv + (long)kh * a.dh;
+  const float c = a.scale * kLog2e;
+  const int window = a.window, sinks = a.sinks;
+
+  bf16x8 kf[NK], vf[NK];
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd) {
+    kf[kd] = row_frag(krow, kd, hh, a.dh);
+    vf[kd] = row_frag(vrow, kd, hh, a.dh);
+  }
+  f32x16 dk[ND], dv[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) { dk[d][e] = 0.f; dv[d][e] = 0.f; }
+
+  // item `it` of the walk: tile walk.t0 + it % nt of head it / nt; (g, t) is the next one to be fetched
+  int g = walk.nt > 0 ? walk.begin / walk.nt : 0, t = walk.nt > 0 ? walk.begin - g * walk.nt : 0;
+  const char *qsrc = uniform_ptr((const char *)((const bf16 *)a.q + (long)b * S * a.ldq + (long)(kh * group + g) * a.dh));
+  const char *osrc = uniform_ptr((const char *)((const bf16 *)a.d_o + (long)b * S * a.ldo + (long)(kh * group + g) * a.dh));
+  const float *lrow = a.lse + ((long)b * a.nq + kh * group + g) * S, *drw = drow + ((long)b * a.nq + kh * group + g) * S;
+  const unsigned ldqb = (unsigned)a.ldq * 2u, ldob = (unsigned)a.ldo * 2u;
+  // the two scalars per query go through a register: even waves carry the 64 log-sum-exps, odd waves the 64 row dots
+  const float *fsrc = (wave & 1) ? drw : lrow;
+  const float fmul = (wave & 1) ? -1.f : kLog2e;   // (dP starts at -D)
+  const float fpad = (wave & 1) ? 0.f : INFINITY;  // (rows past the end: P = 0)
+  float sl = 0.f;
+  int i_next = 0;   // first query of the tile fetched last
+  auto fetch = [&](unsigned buf) {
+    i_next = (walk.t0 + t) * BKV;
+    dma_tile<DH>(buf, qsrc, ldqb, i_next, len, nch, wave, lane);
+    dma_tile<DH>(buf + TILE, osrc, ldob, i_next, len, nch, wave, lane);
+    sl = fsrc[min(i_next + lane, len - 1)];
+    if (++t == walk.nt) { t = 0; qsrc += 2 * a.dh; osrc += 2 * a.dh; fsrc += S; }
+  };
+  auto stash = [&](unsigned stage) {   // [0,64): lse, [64,128): row dots
+    reinterpret_cast<float *>(smem_b + FBASE + stage * FSTAGE)[tid & 127] = i_next + lane < len ? sl * fmul : fpad;
+  };
+  if (walk.begin < walk.end) { fetch(0u); stash(0u); }
+  BothAddr<DH> at;
+  at.init(lane);
+  wait_dma();
+  __syncthreads();
+
+  // the pipeline over the two 32-query sub-tiles A and B of a tile, as in the full attention's dK/dV kernel
+  constexpr int EPS = 16 / NK;
+  bf16x8 fx[2], fy[2];
+  auto ld_rows = [&](int slot, int sub, int kd) {    // Q and dO along the rows: operands of S and dP
+    fx[slot] = at.rows(0u, sub * 32, kd);
+    fy[slot] = at.rows(TILE, sub * 32, kd);
+  };
+  auto ld_cols = [&](int slot, int sub, int j) {     // dO and Q down the rows: operands of dV and dK
+    fx[slot] = at.cols(TILE, sub * 32 + (j / ND) * 16, j % ND);
+    fy[slot] = at.cols(0u, sub * 32 + (j / ND) * 16, j % ND);
+  };
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  auto reads_in = [](auto n_tag) {   // everything read from LDS before the last N reads is in: one wait a step
+    if (DH != 128) return;
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f | (decltype(n_tag)::value << 8));
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  using R0 = std::integral_constant<int, 0>; using R2 = std::integral_constant<int, 2>;
+  using R3 = std::integral_constant<int, 3>; using R4 = std::integral_constant<int, 4>;
+  using R5 = std::integral_constant<int, 5>; using R6 = std::integral_constant<int, 6>;
+  const float *lds_f = reinterpret_cast<const float *>(smem_b + FBASE);   // the current tile's scalars
+  float lsc[2][EPS];
+  auto ld_soft = [&](int q) {
+    const int e0 = (q % NK) * EPS, r0 = (q / NK) * 32 + 8 * (e0 >> 2) + 4 * hh + (e0 & 3);
+    typedef float vec __attribute__((ext_vector_type(EPS)));
+    const vec l = *reinterpret_cast<const vec *>(lds_f + r0);
+#pragma unroll
+    for (int u = 0; u < EPS; ++u) lsc[q & 1][u] = l[u];
+  };
+  auto dp_start = [&](f32x16 &v, const float *scalars, int sub) {   // of sub-tile `sub` of the tile with these scalars
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const f32x4 d = *reinterpret_cast<const f32x4 *>(scalars + BKV + sub * 32 + 8 * e4 + 4 * hh);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[4 * e4 + u] = d[u];
+    }
+  };
+  f32x16 sA, dpA, dpB;
+  auto logits_of_a = [&] {   // stage 4 (and the prologue); leaves the first fragments and scalars of stage 1 in flight
+    ld_rows(0, 0, 0);
+    dp_start(dpA, lds_f, 0);
+    ld_soft(0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sA[e] = 0.f;
+#pragma unroll
+    for (int kd = 0; kd < NK; ++kd) {
+      if (kd + 1 < NK) ld_rows((kd + 1) & 1, 0, kd + 1); else ld_rows((kd + 1) & 1, 1, 0);
+      if (kd == NK - 2) dp_start(dpB, lds_f, 1);
+      if (kd == 0) reads_in(R3{}); else if (kd == NK - 2) reads_in(R6{}); else reads_in(R2{});
+      sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], kf[kd], sA, 0, 0, 0);
+      dpA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], vf[kd], dpA, 0, 0, 0);
+      fence();
+    }
+  };
+
+  unsigned cur = 0;   // the stage at hand
+  auto tile = [&](int i0, auto more_tag) {
+    constexpr bool MORE = decltype(more_tag)::value;
+    const unsigned nxt = cur ^ 1u;
+    if (MORE) fetch(nxt * STAGE);   // (every wave left that stage at the barrier below)
+    auto soft = [&](f32x16 &sv, f32x16 &dpv, int q) {   // logits -> P, dP -> dS
+      const int e0 = (q % NK) * EPS;
+#pragma unroll
+      for (int u = 0; u < EPS; ++u) {
+        const float pr = fast_exp2(sv[e0 + u] * c - lsc[q & 1][u]);
+        sv[e0 + u] = pr;
+        dpv[e0 + u] *= pr;
+      }
+    };
+    auto mask = [&](f32x16 &sv, int sub) {
+      const int ib = i0 + 32 * sub;
+      if (ib < jw0 + 31 || (ib + 31 - jw0 >= window && jw0 + 32 > sinks)) hide(sv, hidden_queries(kj, ib, window, sinks), hh);
+    };
+    f32x16 sB;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sB[e] = 0.f;
+    mask(sA, 0);
+#pragma unroll
+    for (int kd = 0; kd < NK; ++kd) {   // stage 1
+      if (kd + 1 < NK) ld_rows((kd + 1) & 1, 1, kd + 1); else ld_cols((kd + 1) & 1, 0, 0);
+      ld_soft(kd + 1);
+      if (kd + 1 < NK) reads_in(R3{}); else reads_in(R5{});
+      sB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], kf[kd], sB, 0, 0, 0);
+      dpB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], vf[kd], dpB, 0, 0, 0);
+      soft(sA, dpA, kd);
+      fence();
+    }
+    bf16x8 pf[2], dsf[2];
+    pf[0] = pack8(sA, 0); pf[1] = pack8(sA, 8); dsf[0] = pack8(dpA, 0); dsf[1] = pack8(dpA, 8);
+    mask(sB, 1);
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {      // stage 2
+      if (j + 1 < NK) ld_cols((j + 1) & 1, 0, j + 1); else ld_cols((j + 1) & 1, 1, 0);
+      if (j + 1 < NK) ld_soft(NK + j + 1);
+      if (j + 1 < NK) reads_in(R5{}); else reads_in(R4{});
+      dv[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], pf[j / ND], dv[j % ND], 0, 0, 0);
+      dk[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[j & 1], dsf[j / ND], dk[j % ND], 0, 0, 0);
+      soft(sB, dpB, NK + j);
+      fence();
+    }
+    pf[0] = pack8(sB, 0); pf[1] = pack8(sB, 8); dsf[0] = pack8(dpB, 0); dsf[1] = pack8(dpB, 8);
+#pragma unroll
+    for (int j = 0; j < NK; ++j) {      // stage 3
+      if (j + 1 < NK) ld_cols((j + 1) & 1, 1, j + 1);
+      if (j + 1 < NK) reads_in(R4{}); else reads_in(R0{});
+      dv[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], pf[j / ND], dv[j % ND], 0, 0, 0);
+      dk[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[j & 1], dsf[j / ND], dk[j % ND], 0, 0, 0);
+      fence();
+    }
+    if (MORE) stash(nxt);
+    at.flip(STAGE);
+    lds_f = reinterpret_cast<const float *>(smem_b + FBASE + nxt * FSTAGE);
+    wait_dma();
+    __syncthreads();
+    cur = nxt;
+    if (MORE) logits_of_a();   // stage 4
+  };
+  if (walk.begin < walk.end) {
+    logits_of_a();
+    int i0 = i_next;
+    for (int it = walk.begin; it + 1 < walk.end; ++it) {
+      tile(i0, std::true_type{});
+      i0 = i_next;
+    }
+    tile(i0, std::false_type{});
+  }
+
+  if (slot < 0) {
+    unsigned char *ew = smem_b + wave * (128 * DH);
+    store_rows<DH>(ew, dk, a.scale, dkb + (long)jw0 * a.ldk, a.ldk, S - jw0, len - jw0, nch, lane);
+    store_rows<DH>(ew + 64 * DH, dv, 1.f, dvb + (long)jw0 * a.ldv, a.ldv, S - jw0, len - jw0, nch, lane);
+    return;
+  }
+  // sums of this piece: a lane's key is a row, its four consecutive columns one store
+  float *out = sums + slot * (2 * BROWS * DH) + (wave * 32 + (lane & 31)) * DH + 4 * hh;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      f32x4 x, y;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) { x[u] = dk[d][4 * e4 + u]; y[u] = dv[d][4 * e4 + u]; }
+      *reinterpret_cast<f32x4 *>(out + 32 * d + 8 * e4) = x;
+      *reinterpret_cast<f32x4 *>(out + BROWS * DH + 32 * d + 8 * e4) = y;
+    }
+}
+
+// dK, dV of the key blocks whose walk was cut: the pieces' sums, in order.  Block: 32 keys of one of the two.
+template <int DH>
+__global__ __launch_bounds__(256) void window_dkv_sum_kernel(WindowArgs a, KeyWork w, const float *__restrict__ sums, int blocks_per_head) {
+  const int S = a.S, group = a.nq / a.nk, pieces_first = w.parts + w.far;
+  const int quarter = blockIdx.x & 3, which = (blockIdx.x >> 2) & 1, id = blockIdx.x >> 3;
+  const int head = id / blocks_per_head, kb = id - head * blocks_per_head;
+  const int kh = head % a.nk, b = head / a.nk, len = sample_len(a, b);
+  const int pieces = kb < w.first ? pieces_first : w.parts;
+  constexpr int LANES = DH / 4;   // of a row
+  const int col = (threadIdx.x % LANES) * 4;
+  if (col >= a.dh) return;
+  for (int r = threadIdx.x / LANES; r < 32; r += 256 / LANES) {
+    const int row = quarter * 32 + r, j = kb * BROWS + row;
+    if (j >= S) return;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (j < len) {
+      for (int p = 0; p < pieces; ++p) {
+        const Walk walk = walk_of(w, kb, p, len, a.window, group);
+        if (walk.begin == walk.end) continue;
+        s += *reinterpret_cast<const f32x4 *>(sums + slot_of(w, head, kb, p) * (2 * BROWS * DH) + (long)which * BROWS * DH + row * DH + col);
+      }
+    }
+    bf16x4 v;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = (bf16)(which == 0 ? s[u] * a.scale : s[u]);
+    bf16 *out = which == 0 ? (bf16 *)a.dk + ((long)b * S + j) * a.ldk : (bf16 *)a.dv + ((long)b * S + j) * a.ldv;
+    *reinterpret_cast<bf16x4 *>(out + (long)kh * a.dh + col) = v;
+  }
+}
+
+constexpr int kCus = 256;
+
+KeyWork key_work(const WindowArgs &a) {
+  const int group = a.nq / a.nk;
+  KeyWork w;
+  w.key_blocks = (a.S + BROWS - 1) / BROWS;
+  const long blocks = (long)a.B * a.nk * w.key_blocks;
+  const int tiles = (a.S + BKV - 1) / BKV, in_window = (BROWS + a.window - 2) / BKV + 1;   // (as walk_of counts them)
+  const int walk = group * (tiles < in_window ? tiles : in_window);   // items of a block's window, most of them
+  // enough pieces for two blocks a CU, none below eight tiles
+  long parts = (2 * kCus + blocks - 1) / blocks;
+  if (parts > walk / 8) parts = walk / 8;
+  w.parts = parts < 1 ? 1 : (int)parts;
+  const int sinks = a.sinks < a.S ? a.sinks : a.S;
+  const int rest = tiles - in_window;   // tiles past the first block's window
+  w.first = sinks > 0 && rest > 0 ? (sinks + BROWS - 1) / BROWS : 0;
+  const int piece = (walk + w.parts - 1) / w.parts;
+  w.far = w.first > 0 ? (group * rest + piece - 1) / piece : 0;
+  return w;
+}
+size_t slots_of(const WindowArgs &a, const KeyWork &w) {
+  const size_t heads = (size_t)a.B * a.nk;
+  return w.parts == 1 ? heads * w.first * (1 + w.far) : heads * ((size_t)w.key_blocks * w.parts + (size_t)w.first * w.far);
+}
+size_t dots_bytes(const WindowArgs &a) { return ((size_t)a.B * a.nq * a.S * sizeof(float) + 15) & ~(size_t)15; }
+int columns(const WindowArgs &a) { return a.dh <= 64 ? 64 : 128; }
+
+template <typename K> hipError_t with_lds(K kern, size_t smem) {   // (per device and kernel; beyond 64 KB it has to be asked for)
+  return smem <= 64 * 1024 ? hipSuccess
+                           : hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+}
+
+// Blocks of the same weight go head after head; those of a window that most of the sequence fits in are as uneven as a causal
+// mask's and go by weight.
+template <int PER_CU> RowOrder order_of(const WindowArgs &a, int blocks, int tiles, int dh) {
+  return row_order<PER_CU>(2 * (long)a.window >= a.S, blocks, tiles, a.S, dh);
+}
+
+template <int DH> hipError_t fwd_launch(const WindowArgs &a, hipStream_t s) {
+  const int tiles = (a.S + BROWS - 1) / BROWS, blocks = tiles * a.nq * a.B;
+  constexpr size_t smem = 2 * 2 * (size_t)BKV * DH * sizeof(bf16);
+  const RowOrder ro = order_of<DH == 64 ? 3 : 2>(a, blocks, tiles, DH);
+  if (ro.own > 0) hipLaunchKernelGGL((window_fwd_kernel<DH, true>), dim3(blocks), dim3(256), smem, s, a, ro);
+  else hipLaunchKernelGGL((window_fwd_kernel<DH, false>), dim3(blocks), dim3(256), smem, s, a, ro);
+  return hipGetLastError();
+}
+
+template <int DH> hipError_t bwd_launch(const WindowArgs &a, hipStream_t s) {
+  const int tiles = (a.S + BROWS - 1) / BROWS, blocks_q = tiles * a.nq * a.B;
+  constexpr size_t smem_q = 2 * 2 * (size_t)BKV * DH * sizeof(bf16);
+  constexpr size_t smem_k = 2 * (2 * (size_t)BKV * DH * sizeof(bf16) + 2 * BKV * sizeof(float));
+  const KeyWork w = key_work(a);
+  hipError_t e = with_lds(window_dkv_kernel<DH>, smem_k);
+  if (e != hipSuccess) return e;
+  // dQ first: it leaves the row dots <dO_i, O_i> in the workspace
+  const RowOrder ro = order_of<2>(a, blocks_q, tiles, DH);
+  if (ro.own > 0) hipLaunchKernelGGL((window_dq_kernel<DH, true>), dim3(blocks_q), dim3(256), smem_q, s, a, ro);
+  else hipLaunchKernelGGL((window_dq_kernel<DH, false>), dim3(blocks_q), dim3(256), smem_q, s, a, ro);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  float *sums = (float *)((char *)a.ws + dots_bytes(a));
+  const int heads = a.B * a.nk, blocks_k = heads * (w.key_blocks * w.parts + w.first * w.far);
+  hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3(blocks_k), dim3(256), smem_k, s, a, w, a.ws, sums);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int cut = w.parts > 1 ? w.key_blocks : w.first;   // key blocks a head with several pieces
+  if (cut == 0) return hipSuccess;
+  hipLaunchKernelGGL((window_dkv_sum_kernel<DH>), dim3(heads * cut * 8), dim3(256), 0, s, a, w, sums, cut);
+  return hipGetLastError();
+}
+
+bool fits(const void *p, long ld, int S) {
+  return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && (uint64_t)S * (uint64_t)ld * 2 < 0xffffffffull - 4096;
+}
+
+}  // namespace
+
+bool window_mfma_supported(const WindowArgs &a) {
+  return a.dh <= 128 && fits(a.q, a.ldq, a.S) && fits(a.k, a.ldk, a.S) && fits(a.v, a.ldv, a.S) && fits(a.o, a.ldo, a.S) &&
+         fits(a.o_in, a.ldo, a.S) && fits(a.d_o, a.ldo, a.S) && fits(a.dq, a.ldq, a.S) && fits(a.dk, a.ldk, a.S) && fits(a.dv, a.ldv, a.S) &&
+         ((uintptr_t)a.ws & 15) == 0;
+}
+size_t window_mfma_ws_bytes(const WindowArgs &a) {
+  return a.dh > 128 ? 0 : dots_bytes(a) + slots_of(a, key_work(a)) * 2 * BROWS * (size_t)columns(a) * sizeof(float);
+}
+hipError_t launch_window_fwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? fwd_launch<64>(a, s) : fwd_launch<128>(a, s); }
+hipError_t launch_window_bwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? bwd_launch<64>(a, s) : bwd_launch<128>(a, s); }
+
+}  // namespace dp

@@ -209,8 +209,23 @@ hipError_t launch_window_bwd_simple(int dtype, const WindowArgs &a, hipStream_t 
 }
 
 // ---- which kernels a call runs
-size_t window_ws_bytes(int, const WindowArgs &a) { return (size_t)a.B * a.nq * a.S * sizeof(float); }
-hipError_t launch_window_fwd(int dtype, const WindowArgs &a, hipStream_t s) { return launch_window_fwd_simple(dtype, a, s); }
-hipError_t launch_window_bwd(int dtype, const WindowArgs &a, hipStream_t s) { return launch_window_bwd_simple(dtype, a, s); }
+static WindowArgs clipped(WindowArgs a) {   // a window, or first keys, beyond the sequence: all of it
+  if (a.window > a.S) a.window = a.S;
+  if (a.sinks > a.S) a.sinks = a.S;
+  return a;
+}
+size_t window_ws_bytes(int dtype, const WindowArgs &args) {
+  const WindowArgs a = clipped(args);
+  const size_t simple = (size_t)a.B * a.nq * a.S * sizeof(float), mfma = dtype == kBF16 && a.S > 0 ? window_mfma_ws_bytes(a) : 0;
+  return simple > mfma ? simple : mfma;
+}
+hipError_t launch_window_fwd(int dtype, const WindowArgs &args, hipStream_t s) {
+  const WindowArgs a = clipped(args);
+  return dtype == kBF16 && window_mfma_supported(a) ? launch_window_fwd_mfma(a, s) : launch_window_fwd_simple(dtype, a, s);
+}
+hipError_t launch_window_bwd(int dtype, const WindowArgs &args, hipStream_t s) {
+  const WindowArgs a = clipped(args);
+  return dtype == kBF16 && window_mfma_supported(a) ? launch_window_bwd_mfma(a, s) : launch_window_bwd_simple(dtype, a, s);
+}
 
 }  // namespace dp
