@@ -683,8 +683,8 @@ dp_status dp_op_qk_rotary_bwd(int32_t dtype, const dp_qk_rotary *shape, const vo
  * length become 0); ws: device workspace of dp_op_window_attention_workspace_bytes bytes.  No
  * overlap of an output with anything.  Sums and statistics fp32, results rounded once (in bf16 the
  * probabilities and the logits' gradients are rounded to bf16 for the products they go into); the
- * same bits at every call.  In bf16 a key or value that is not finite may spread to any row of its
- * sample, not to other samples.  head_dim is a multiple of 8 and at most 256 (DP_E_UNSUPPORTED
+ * same bits at every call.  A key or value that is not finite may spread to any row of its sample
+ * (hidden keys meet it with a weight of zero), not to other samples.  head_dim is a multiple of 8 and at most 256 (DP_E_UNSUPPORTED
  * otherwise).  Any alignment; the matrix cores take head dimensions up to 128 with pointers 16-byte
  * aligned, strides that are multiples of 16 bytes and samples that span less than 4 GiB, everything
  * else goes to vector-ALU kernels 20 to 100 times slower. */

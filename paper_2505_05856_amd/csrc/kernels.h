@@ -207,6 +207,10 @@ bool window_mfma_supported(const WindowArgs &a);
 size_t window_mfma_ws_bytes(const WindowArgs &a);
 hipError_t launch_window_fwd_mfma(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_bwd_mfma(const WindowArgs &a, hipStream_t s);
+bool window_f32_supported(const WindowArgs &a);         // fp32 on the matrix cores, likewise
+size_t window_f32_ws_bytes(const WindowArgs &a);
+hipError_t launch_window_fwd_f32(const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_bwd_f32(const WindowArgs &a, hipStream_t s);
 
 // ---- norms of queries and keys with rotary positions ---------------------------------------------
 // nq query and nk key heads of dh elements in rows of the given strides; forward q, k -> q_out, k_out, backward dq_out, dk_out

@@ -12,51 +12,13 @@
 // - Rows past a sample's length are never read (tiles end with copies of the last row, whose products are masked) and become 0.
 // - Head dimensions of 8..128: kernels for 64 and 128 columns; columns past the head are zeros on the side that waits in
 //   registers and copies of the first ones in LDS, and are not stored.
-#include "attn_tile.h"
+#include "window_tile.h"
 
 #include <type_traits>
 
 namespace dp {
 
 namespace {
-
-// ---- what a query, or a key, sees ------------------------------------------------------------------
-// bits x and up of a 32-bit word (any x)
-__device__ __forceinline__ uint32_t bits_from(int x) { return (uint32_t)(0xffffffffull << min(max(x, 0), 32)); }
-// the hidden ones of keys jb .. jb+31 for query i
-__device__ __forceinline__ uint32_t hidden_keys(int i, int jb, int window, int sinks) {
-  return bits_from(i + 1 - jb) | (bits_from(sinks - jb) & ~bits_from(i - window + 1 - jb));
-}
-// the hidden ones of queries ib .. ib+31 for key j
-__device__ __forceinline__ uint32_t hidden_queries(int j, int ib, int window, int sinks) {
-  return ~bits_from(j - ib) | (j < sinks ? 0u : bits_from(j + window - ib));
-}
-// -inf for the hidden ones of a 32x32 result's 16 elements a lane (rows acc_row(e, lane))
-__device__ __forceinline__ void hide(f32x16 &v, uint32_t hidden, int hh) {
-  const int h = (int)(hidden >> (4 * hh));
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int m = __builtin_amdgcn_sbfe(h, 8 * (e >> 2) + (e & 3), 1);   // all ones where hidden
-    v[e] = __int_as_float((m & 0xff800000) | (~m & __float_as_int(v[e])));
-  }
-}
-
-// The key tiles (64 keys) that a block of queries q0 .. q0+127 walks: the first `head` tiles, then tiles from `from` on.
-struct KeyTiles {
-  int head, gap, n;   // n: how many in all; tile t of the walk is t, or t + gap from `head` on
-  __device__ __forceinline__ KeyTiles(int q0, int len, int window, int sinks) {
-    const int end = (min(q0 + BROWS, len) - 1) / BKV + 1, w0 = max(q0 - window + 1, 0) / BKV;
-    head = min((sinks + BKV - 1) / BKV, w0);
-    gap = w0 - head;
-    n = end - gap;
-  }
-  __device__ __forceinline__ int first_key(int t) const { return (t < head ? t : t + gap) * BKV; }
-};
-
-// Rows of sample b that hold a sequence (the same in every lane, and known to be)
-__device__ __forceinline__ int sample_len(const WindowArgs &a, int b) {
-  return __builtin_amdgcn_readfirstlane(window_len(a, a.lens != nullptr ? a.lens[b] : 0));
-}
 
 // ---- tiles whose heads may be narrower than the kernel ---------------------------------------------------
 // request i of the DH/32 a wave issues for a tile (as dma_req_both): chunks past the head's `nch` read its first
@@ -144,7 +106,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void window_fwd_kernel(Windo
   const unsigned ldkb = (unsigned)a.ldk * 2u, ldvb = (unsigned)a.ldv * 2u;
   const float c = a.scale * kLog2e;
   const int window = a.window, sinks = a.sinks;
-  const KeyTiles kt(q0, len, window, sinks);
+  const KeyTiles<BKV, BROWS> kt(q0, len, window, sinks);
   // whether tile t of the walk hides a key from a query of the block
   auto hides = [&](int t) {
     const int j0 = kt.first_key(t);
@@ -323,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
   const int iw0 = q0 + wave * 32, qi = iw0 + (lane & 31);
   const float c = a.scale * kLog2e;
   const int window = a.window, sinks = a.sinks;
-  const KeyTiles kt(q0, len, window, sinks);
+  const KeyTiles<BKV, BROWS> kt(q0, len, window, sinks);
   auto fetch = [&](int t, unsigned buf) {
     const int j0 = kt.first_key(t);
     dma_tile<DH>(buf, ksrc, ldkb, j0, len, nch, wave, lane);
@@ -444,34 +406,6 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
 }
 
 // ------------------------------------------------------------------ backward: dK and dV
-// How the walks over query tiles (64 queries) are cut.  Key block kb (128 keys) of a key head walks, for each query head of its
-// group, the tiles from its own first to the end of its window: `parts` pieces.  Key blocks below `first` hold keys that all
-// later queries see: the rest of the sequence, `far` pieces more.
-struct KeyWork { int key_blocks, parts, first, far; };
-
-struct Walk { int t0, nt, begin, end; };   // query tiles t0 .. t0+nt-1 of each head in turn; items begin .. end-1 of that list
-__host__ __device__ __forceinline__ Walk walk_of(const KeyWork &w, int kb, int piece, int len, int window, int group) {
-  const int tiles = (len + BKV - 1) / BKV, t0 = 2 * kb;
-  const long last = ((long)kb * BROWS + BROWS - 1 + window - 1) / BKV;   // the last tile of the window
-  const int t1 = last + 1 < tiles ? (int)last + 1 : tiles;
-  Walk r;
-  const bool far = piece >= w.parts;
-  r.t0 = far ? (t1 > t0 ? t1 : t0) : t0;
-  const int end = far ? tiles : t1;
-  r.nt = end > r.t0 ? end - r.t0 : 0;
-  const int n = r.nt * group, pieces = far ? w.far : w.parts, chunk = (n + pieces - 1) / pieces, i = far ? piece - w.parts : piece;
-  r.begin = i * chunk < n ? i * chunk : n;
-  r.end = r.begin + chunk < n ? r.begin + chunk : n;
-  return r;
-}
-// Where a piece's sums go: a slot of the workspace (two [128][DH] arrays), or -1: it is its block's only one, the result itself.
-__host__ __device__ __forceinline__ long slot_of(const KeyWork &w, long head, int kb, int piece) {
-  const int sinks_at = w.key_blocks * w.parts;   // slots a head: those of the windows, where they have several, then the far ones
-  if (w.parts == 1) return kb >= w.first ? -1 : head * (long)w.first * (1 + w.far) + (long)kb * (1 + w.far) + piece;
-  return head * ((long)sinks_at + (long)w.first * w.far) +
-         (piece < w.parts ? (long)kb * w.parts + piece : sinks_at + (long)kb * w.far + piece - w.parts);
-}
-
 template <int DH>
 __global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
                                                                           float *__restrict__ sums) {
@@ -501,7 +435,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void window_dkv_kernel(Wind
     }
     return;
   }
-  const Walk walk = walk_of(w, kb, piece, len, a.window, group);
+  const Walk walk = walk_of<BROWS>(w, kb, piece, len, a.window, group);
   if (slot >= 0 && walk.begin == walk.end) return;   // (the kernel that adds the pieces up knows)
   const bf16 *krow = (const bf16 *)a.k + ((long)b * S + min(kj, len - 1)) * a.ldk + (long)kh * a.dh;
   const bf16 *vrow = (const bf16 *)a.v + ((long)b * S + min(kj, len - 1)) * a.ldv + (long)kh * a.dh;
@@ -696,62 +630,10 @@ __global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void window_dkv_kernel(Wind
     }
 }
 
-// dK, dV of the key blocks whose walk was cut: the pieces' sums, in order.  Block: 32 keys of one of the two.
-template <int DH>
-__global__ __launch_bounds__(256) void window_dkv_sum_kernel(WindowArgs a, KeyWork w, const float *__restrict__ sums, int blocks_per_head) {
-  const int S = a.S, group = a.nq / a.nk, pieces_first = w.parts + w.far;
-  const int quarter = blockIdx.x & 3, which = (blockIdx.x >> 2) & 1, id = blockIdx.x >> 3;
-  const int head = id / blocks_per_head, kb = id - head * blocks_per_head;
-  const int kh = head % a.nk, b = head / a.nk, len = sample_len(a, b);
-  const int pieces = kb < w.first ? pieces_first : w.parts;
-  constexpr int LANES = DH / 4;   // of a row
-  const int col = (threadIdx.x % LANES) * 4;
-  if (col >= a.dh) return;
-  for (int r = threadIdx.x / LANES; r < 32; r += 256 / LANES) {
-    const int row = quarter * 32 + r, j = kb * BROWS + row;
-    if (j >= S) return;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (j < len) {
-      for (int p = 0; p < pieces; ++p) {
-        const Walk walk = walk_of(w, kb, p, len, a.window, group);
-        if (walk.begin == walk.end) continue;
-        s += *reinterpret_cast<const f32x4 *>(sums + slot_of(w, head, kb, p) * (2 * BROWS * DH) + (long)which * BROWS * DH + row * DH + col);
-      }
-    }
-    bf16x4 v;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = (bf16)(which == 0 ? s[u] * a.scale : s[u]);
-    bf16 *out = which == 0 ? (bf16 *)a.dk + ((long)b * S + j) * a.ldk : (bf16 *)a.dv + ((long)b * S + j) * a.ldv;
-    *reinterpret_cast<bf16x4 *>(out + (long)kh * a.dh + col) = v;
-  }
-}
-
-constexpr int kCus = 256;
-
-KeyWork key_work(const WindowArgs &a) {
-  const int group = a.nq / a.nk;
-  KeyWork w;
-  w.key_blocks = (a.S + BROWS - 1) / BROWS;
-  const long blocks = (long)a.B * a.nk * w.key_blocks;
-  const int tiles = (a.S + BKV - 1) / BKV, in_window = (BROWS + a.window - 2) / BKV + 1;   // (as walk_of counts them)
-  const int walk = group * (tiles < in_window ? tiles : in_window);   // items of a block's window, most of them
-  // enough pieces for two blocks a CU, none below eight tiles
-  long parts = (2 * kCus + blocks - 1) / blocks;
-  if (parts > walk / 8) parts = walk / 8;
-  w.parts = parts < 1 ? 1 : (int)parts;
-  const int sinks = a.sinks < a.S ? a.sinks : a.S;
-  const int rest = tiles - in_window;   // tiles past the first block's window
-  w.first = sinks > 0 && rest > 0 ? (sinks + BROWS - 1) / BROWS : 0;
-  const int piece = (walk + w.parts - 1) / w.parts;
-  w.far = w.first > 0 ? (group * rest + piece - 1) / piece : 0;
-  return w;
-}
-size_t slots_of(const WindowArgs &a, const KeyWork &w) {
-  const size_t heads = (size_t)a.B * a.nk;
-  return w.parts == 1 ? heads * w.first * (1 + w.far) : heads * ((size_t)w.key_blocks * w.parts + (size_t)w.first * w.far);
-}
-size_t dots_bytes(const WindowArgs &a) { return ((size_t)a.B * a.nq * a.S * sizeof(float) + 15) & ~(size_t)15; }
 int columns(const WindowArgs &a) { return a.dh <= 64 ? 64 : 128; }
+
+// (blocks at once: one a CU at 128 columns, two at 64)
+KeyWork work_of(const WindowArgs &a) { return key_work<BROWS>(a, columns(a) == 128 ? kCus : 2 * kCus); }
 
 template <typename K> hipError_t with_lds(K kern, size_t smem) {   // (per device and kernel; beyond 64 KB it has to be asked for)
   return smem <= 64 * 1024 ? hipSuccess
@@ -777,7 +659,7 @@ template <int DH> hipError_t bwd_launch(const WindowArgs &a, hipStream_t s) {
   const int tiles = (a.S + BROWS - 1) / BROWS, blocks_q = tiles * a.nq * a.B;
   constexpr size_t smem_q = 2 * 2 * (size_t)BKV * DH * sizeof(bf16);
   constexpr size_t smem_k = 2 * (2 * (size_t)BKV * DH * sizeof(bf16) + 2 * BKV * sizeof(float));
-  const KeyWork w = key_work(a);
+  const KeyWork w = work_of(a);
   hipError_t e = with_lds(window_dkv_kernel<DH>, smem_k);
   if (e != hipSuccess) return e;
   // dQ first: it leaves the row dots <dO_i, O_i> in the workspace
@@ -786,12 +668,12 @@ template <int DH> hipError_t bwd_launch(const WindowArgs &a, hipStream_t s) {
   else hipLaunchKernelGGL((window_dq_kernel<DH, false>), dim3(blocks_q), dim3(256), smem_q, s, a, ro);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   float *sums = (float *)((char *)a.ws + dots_bytes(a));
-  const int heads = a.B * a.nk, blocks_k = heads * (w.key_blocks * w.parts + w.first * w.far);
-  hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3(blocks_k), dim3(256), smem_k, s, a, w, a.ws, sums);
+  const int heads = a.B * a.nk;
+  hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3((unsigned)(heads * pieces_of(w))), dim3(256), smem_k, s, a, w, a.ws, sums);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  const int cut = w.parts > 1 ? w.key_blocks : w.first;   // key blocks a head with several pieces
+  const int cut = key_blocks_cut(w);
   if (cut == 0) return hipSuccess;
-  hipLaunchKernelGGL((window_dkv_sum_kernel<DH>), dim3(heads * cut * 8), dim3(256), 0, s, a, w, sums, cut);
+  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, BROWS, DH>), dim3(heads * cut * 2 * (BROWS / 32)), dim3(256), 0, s, a, w, sums, cut);
   return hipGetLastError();
 }
 
@@ -807,7 +689,7 @@ bool window_mfma_supported(const WindowArgs &a) {
          ((uintptr_t)a.ws & 15) == 0;
 }
 size_t window_mfma_ws_bytes(const WindowArgs &a) {
-  return a.dh > 128 ? 0 : dots_bytes(a) + slots_of(a, key_work(a)) * 2 * BROWS * (size_t)columns(a) * sizeof(float);
+  return a.dh > 128 ? 0 : dots_bytes(a) + slots_of(a, work_of(a)) * 2 * BROWS * (size_t)columns(a) * sizeof(float);
 }
 hipError_t launch_window_fwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? fwd_launch<64>(a, s) : fwd_launch<128>(a, s); }
 hipError_t launch_window_bwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? bwd_launch<64>(a, s) : bwd_launch<128>(a, s); }

@@ -209,23 +209,27 @@ hipError_t launch_window_bwd_simple(int dtype, const WindowArgs &a, hipStream_t 
 }
 
 // ---- which kernels a call runs
-static WindowArgs clipped(WindowArgs a) {   // a window, or first keys, beyond the sequence: all of it
-  if (a.window > a.S) a.window = a.S;
-  if (a.sinks > a.S) a.sinks = a.S;
+static WindowArgs clipped(WindowArgs a) {   // a window that with the first keys covers the sequence: all of it
+  if ((long)a.window + a.sinks >= a.S) { a.window = a.S; a.sinks = 0; }
   return a;
 }
 size_t window_ws_bytes(int dtype, const WindowArgs &args) {
   const WindowArgs a = clipped(args);
-  const size_t simple = (size_t)a.B * a.nq * a.S * sizeof(float), mfma = dtype == kBF16 && a.S > 0 ? window_mfma_ws_bytes(a) : 0;
-  return simple > mfma ? simple : mfma;
+  const size_t simple = (size_t)a.B * a.nq * a.S * sizeof(float);
+  const size_t matrix = a.S == 0 ? 0 : dtype == kBF16 ? window_mfma_ws_bytes(a) : window_f32_ws_bytes(a);
+  return simple > matrix ? simple : matrix;
 }
 hipError_t launch_window_fwd(int dtype, const WindowArgs &args, hipStream_t s) {
   const WindowArgs a = clipped(args);
-  return dtype == kBF16 && window_mfma_supported(a) ? launch_window_fwd_mfma(a, s) : launch_window_fwd_simple(dtype, a, s);
+  if (dtype == kBF16 && window_mfma_supported(a)) return launch_window_fwd_mfma(a, s);
+  if (dtype == kF32 && window_f32_supported(a)) return launch_window_fwd_f32(a, s);
+  return launch_window_fwd_simple(dtype, a, s);
 }
 hipError_t launch_window_bwd(int dtype, const WindowArgs &args, hipStream_t s) {
   const WindowArgs a = clipped(args);
-  return dtype == kBF16 && window_mfma_supported(a) ? launch_window_bwd_mfma(a, s) : launch_window_bwd_simple(dtype, a, s);
+  if (dtype == kBF16 && window_mfma_supported(a)) return launch_window_bwd_mfma(a, s);
+  if (dtype == kF32 && window_f32_supported(a)) return launch_window_bwd_f32(a, s);
+  return launch_window_bwd_simple(dtype, a, s);
 }
 
 }  // namespace dp
