@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdpstage.so")
-SOURCES = ["stage.cpp", "planner.cpp", "ops.cpp", "elementwise.hip", "gemm_simple.hip", "gemm_f32.hip", "attn_simple.hip", "gemm_mfma.hip", "gemm_dma.hip", "gemm_pair.hip", "attn_mfma.hip", "rotary.hip", "window_simple.hip", "window_mfma.hip", "window_f32.hip", "probe.hip"]
+SOURCES = ["stage.cpp", "planner.cpp", "ops.cpp", "elementwise.hip", "gemm_simple.hip", "gemm_f32.hip", "attn_simple.hip", "gemm_mfma.hip", "gemm_dma.hip", "gemm_pair.hip", "attn_mfma.hip", "rotary.hip", "window_simple.hip", "window_mfma.hip", "window_dkv.hip", "window_f32.hip", "probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
@@ -30,7 +30,7 @@ NO_SCRATCH = {"gemm_mfma.hip", "gemm_dma.hip", "gemm_pair.hip"}
 # registers for them removes nearly all of those moves.
 EXTRA_FLAGS = {"attn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-inline-asm"],
                # (the same pipelines)
-               "window_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-inline-asm"], "window_f32.hip": ["-Wno-inline-asm"],
+               "window_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-inline-asm"], "window_f32.hip": ["-Wno-inline-asm"], "window_dkv.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-inline-asm"],
                # the LDS-direct load names M0 as clobbered; clang warns that M0 is a reserved register
                "gemm_dma.hip": ["-Wno-inline-asm"], "gemm_pair.hip": ["-Wno-inline-asm"]}
 
@@ -39,7 +39,7 @@ EXTRA_FLAGS = {"attn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-inlin
 # register the compiler also uses by itself (LDS-indexed operations, lane moves, spill code) without modelling
 # inline asm's writes: such a use next to the loads would be a silent miscompile.  The device assembly of these
 # files must therefore name M0 only inside the inline asm blocks.
-M0_BY_HAND = {"gemm_dma.hip", "gemm_pair.hip", "attn_mfma.hip", "window_mfma.hip"}
+M0_BY_HAND = {"gemm_dma.hip", "gemm_pair.hip", "attn_mfma.hip", "window_mfma.hip", "window_dkv.hip"}
 
 
 def device_asm(src: str, asm: str) -> None:

@@ -12,67 +12,13 @@
 // - Rows past a sample's length are never read (tiles end with copies of the last row, whose products are masked) and become 0.
 // - Head dimensions of 8..128: kernels for 64 and 128 columns; columns past the head are zeros on the side that waits in
 //   registers and copies of the first ones in LDS, and are not stored.
-#include "window_tile.h"
+#include "window_bf16.h"
 
 #include <type_traits>
 
 namespace dp {
 
 namespace {
-
-// ---- tiles whose heads may be narrower than the kernel ---------------------------------------------------
-// request i of the DH/32 a wave issues for a tile (as dma_req_both): chunks past the head's `nch` read its first
-template <int DH>
-__device__ __forceinline__ void dma_req(int i, unsigned lds_byte, const char *src, unsigned ldb, int row0, int nrows, int nch, int wave,
-                                        int lane) {
-  constexpr int NREQ = DH / 32, RPR = 1024 / (DH * 2), CPR = DH / 8;
-  const int q = wave * NREQ + i, r = RPR * q + lane / CPR;
-  const int rg = min(row0 + r, nrows - 1);
-  const int chunk = (int)((unsigned)(lane % CPR) ^ swz_both<DH>((unsigned)r));
-  dma16(lds_byte + (unsigned)q * 1024u, (unsigned)rg * ldb + (unsigned)(chunk < nch ? chunk : 0) * 16u, src);
-}
-template <int DH>
-__device__ __forceinline__ void dma_tile(unsigned lds_byte, const char *src, unsigned ldb, int row0, int nrows, int nch, int wave, int lane) {
-#pragma unroll
-  for (int i = 0; i < DH / 32; ++i) dma_req<DH>(i, lds_byte, src, ldb, row0, nrows, nch, wave, lane);
-}
-// elements 16 kd + 8 (lane / 32) .. of a row as an operand fragment, zeros past the head
-__device__ __forceinline__ bf16x8 row_frag(const bf16 *row, int kd, int hh, int dh) {
-  const int at = kd * 16 + 8 * hh;
-  const uint4 v = ld16(row + (at < dh ? at : 0));   // (unguarded: the compiler would wait for each load on its own)
-  return as_frag(at < dh ? v : make_uint4(0u, 0u, 0u, 0u));
-}
-// as store_rows_via_lds, for heads of `nch` 16-byte chunks; rows from `valid` on become zeros
-template <int DH>
-__device__ __forceinline__ void store_rows(unsigned char *ew, const f32x16 (&acc)[DH / 32], float mul, bf16 *dst, long ld, int nrows,
-                                           int valid, int nch, int lane) {
-  constexpr int ND = DH / 32, CPR = DH / 8, RPI = 64 / CPR;
-  const int row = lane & 31, hh = lane >> 5;
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) {
-      bf16x4 v;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) v[t] = (bf16)(acc[d][e4 * 4 + t] * mul);
-      const int pos = (d * 4 + e4) ^ (row & (CPR - 1));
-      *reinterpret_cast<bf16x4 *>(ew + row * (DH * 2) + pos * 16 + hh * 8) = v;
-    }
-#pragma unroll
-  for (int i = 0; i < 32 / RPI; ++i) {
-    const int r = i * RPI + lane / CPR, c = lane % CPR;
-    uint4 q = *reinterpret_cast<const uint4 *>(ew + r * (DH * 2) + ((c ^ (r & (CPR - 1))) * 16));
-    if (r >= valid) q = make_uint4(0u, 0u, 0u, 0u);
-    if (r < nrows && c < nch) *reinterpret_cast<uint4 *>(dst + (long)r * ld + c * 8) = q;
-  }
-}
-// rows r0 .. r1-1 of a head become zeros (by the whole block)
-__device__ __forceinline__ void zero_rows(bf16 *dst, long ld, int r0, int r1, int nch) {
-  for (int i = threadIdx.x; i < (r1 - r0) * nch; i += 256) {
-    const int r = r0 + i / nch, c = i % nch;
-    *reinterpret_cast<uint4 *>(dst + (long)r * ld + c * 8) = make_uint4(0u, 0u, 0u, 0u);
-  }
-}
 
 // ------------------------------------------------------------------ forward
 // The pipeline of a tile is the full attention's (attn_mfma.hip): the logits of tile t+1 are taken beside the softmax of tile t.
@@ -405,240 +351,6 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
   store_rows<DH>(smem_b + wave * (64 * DH), dq, a.scale, dqb + (long)iw0 * a.ldq, a.ldq, S - iw0, len - iw0, nch, lane);
 }
 
-// ------------------------------------------------------------------ backward: dK and dV
-template <int DH>
-__global__ __launch_bounds__(256, DH == 128 ? 1 : 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
-                                                                          float *__restrict__ sums) {
-  constexpr int ND = DH / 32, NK = DH / 16;
-  // LDS, in bytes: [stage 0: Q, dO][stage 1: Q, dO][stage 0: lse, row dots][stage 1: lse, row dots]
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
-  constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE, FBASE = 2 * STAGE, FSTAGE = 8 * BKV;
-
-  const int S = a.S, nch = a.dh / 8, group = a.nq / a.nk;
-  // a head's pieces: the far ones first, then the windows' from the first key block on
-  const int per_head = w.key_blocks * w.parts + w.first * w.far;
-  const int wid = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int head = wid / per_head, id = wid - head * per_head, nfar = w.first * w.far;
-  const int kb = id < nfar ? id / w.far : (id - nfar) / w.parts;
-  const int piece = id < nfar ? w.parts + id % w.far : (id - nfar) % w.parts;
-  const int kh = head % a.nk, b = head / a.nk;
-  const int len = sample_len(a, b);
-  const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int j0 = kb * BROWS, jw0 = j0 + wave * 32, kj = jw0 + (lane & 31);
-  const long slot = slot_of(w, head, kb, piece);
-  bf16 *dkb = (bf16 *)a.dk + (long)b * S * a.ldk + (long)kh * a.dh, *dvb = (bf16 *)a.dv + (long)b * S * a.ldv + (long)kh * a.dh;
-  if (j0 >= len) {
-    if (slot < 0) {
-      zero_rows(dkb, a.ldk, j0, min(j0 + BROWS, S), nch);
-      zero_rows(dvb, a.ldv, j0, min(j0 + BROWS, S), nch);
-    }
-    return;
-  }
-  const Walk walk = walk_of<BROWS>(w, kb, piece, len, a.window, group);
-  if (slot >= 0 && walk.begin == walk.end) return;   // (the kernel that adds the pieces up knows)
-  const bf16 *krow = (const bf16 *)a.k + ((long)b * S + min(kj, len - 1)) * a.ldk + (long)kh * a.dh;
-  const bf16 *vrow = (const bf16 *)a.v + ((long)b * S + min(kj, len - 1)) * a.ldv + (long)kh * a.dh;
-  const float c = a.scale * kLog2e;
-  const int window = a.window, sinks = a.sinks;
-
-  bf16x8 kf[NK], vf[NK];
-#pragma unroll
-  for (int kd = 0; kd < NK; ++kd) {
-    kf[kd] = row_frag(krow, kd, hh, a.dh);
-    vf[kd] = row_frag(vrow, kd, hh, a.dh);
-  }
-  f32x16 dk[ND], dv[ND];
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) { dk[d][e] = 0.f; dv[d][e] = 0.f; }
-
-  // item `it` of the walk: tile walk.t0 + it % nt of head it / nt; (g, t) is the next one to be fetched
-  int g = walk.nt > 0 ? walk.begin / walk.nt : 0, t = walk.nt > 0 ? walk.begin - g * walk.nt : 0;
-  const char *qsrc = uniform_ptr((const char *)((const bf16 *)a.q + (long)b * S * a.ldq + (long)(kh * group + g) * a.dh));
-  const char *osrc = uniform_ptr((const char *)((const bf16 *)a.d_o + (long)b * S * a.ldo + (long)(kh * group + g) * a.dh));
-  const float *lrow = a.lse + ((long)b * a.nq + kh * group + g) * S, *drw = drow + ((long)b * a.nq + kh * group + g) * S;
-  const unsigned ldqb = (unsigned)a.ldq * 2u, ldob = (unsigned)a.ldo * 2u;
-  // the two scalars per query go through a register: even waves carry the 64 log-sum-exps, odd waves the 64 row dots
-  const float *fsrc = (wave & 1) ? drw : lrow;
-  const float fmul = (wave & 1) ? -1.f : kLog2e;   // (dP starts at -D)
-  const float fpad = (wave & 1) ? 0.f : INFINITY;  // (rows past the end: P = 0)
-  float sl = 0.f;
-  int i_next = 0;   // first query of the tile fetched last
-  auto fetch = [&](unsigned buf) {
-    i_next = (walk.t0 + t) * BKV;
-    dma_tile<DH>(buf, qsrc, ldqb, i_next, len, nch, wave, lane);
-    dma_tile<DH>(buf + TILE, osrc, ldob, i_next, len, nch, wave, lane);
-    sl = fsrc[min(i_next + lane, len - 1)];
-    if (++t == walk.nt) { t = 0; qsrc += 2 * a.dh; osrc += 2 * a.dh; fsrc += S; }
-  };
-  auto stash = [&](unsigned stage) {   // [0,64): lse, [64,128): row dots
-    reinterpret_cast<float *>(smem_b + FBASE + stage * FSTAGE)[tid & 127] = i_next + lane < len ? sl * fmul : fpad;
-  };
-  if (walk.begin < walk.end) { fetch(0u); stash(0u); }
-  BothAddr<DH> at;
-  at.init(lane);
-  wait_dma();
-  __syncthreads();
-
-  // the pipeline over the two 32-query sub-tiles A and B of a tile, as in the full attention's dK/dV kernel
-  constexpr int EPS = 16 / NK;
-  bf16x8 fx[2], fy[2];
-  auto ld_rows = [&](int slot, int sub, int kd) {    // Q and dO along the rows: operands of S and dP
-    fx[slot] = at.rows(0u, sub * 32, kd);
-    fy[slot] = at.rows(TILE, sub * 32, kd);
-  };
-  auto ld_cols = [&](int slot, int sub, int j) {     // dO and Q down the rows: operands of dV and dK
-    fx[slot] = at.cols(TILE, sub * 32 + (j / ND) * 16, j % ND);
-    fy[slot] = at.cols(0u, sub * 32 + (j / ND) * 16, j % ND);
-  };
-  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-  auto reads_in = [](auto n_tag) {   // everything read from LDS before the last N reads is in: one wait a step
-    if (DH != 128) return;
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0xc07f | (decltype(n_tag)::value << 8));
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  using R0 = std::integral_constant<int, 0>; using R2 = std::integral_constant<int, 2>;
-  using R3 = std::integral_constant<int, 3>; using R4 = std::integral_constant<int, 4>;
-  using R5 = std::integral_constant<int, 5>; using R6 = std::integral_constant<int, 6>;
-  const float *lds_f = reinterpret_cast<const float *>(smem_b + FBASE);   // the current tile's scalars
-  float lsc[2][EPS];
-  auto ld_soft = [&](int q) {
-    const int e0 = (q % NK) * EPS, r0 = (q / NK) * 32 + 8 * (e0 >> 2) + 4 * hh + (e0 & 3);
-    typedef float vec __attribute__((ext_vector_type(EPS)));
-    const vec l = *reinterpret_cast<const vec *>(lds_f + r0);
-#pragma unroll
-    for (int u = 0; u < EPS; ++u) lsc[q & 1][u] = l[u];
-  };
-  auto dp_start = [&](f32x16 &v, const float *scalars, int sub) {   // of sub-tile `sub` of the tile with these scalars
-#pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) {
-      const f32x4 d = *reinterpret_cast<const f32x4 *>(scalars + BKV + sub * 32 + 8 * e4 + 4 * hh);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[4 * e4 + u] = d[u];
-    }
-  };
-  f32x16 sA, dpA, dpB;
-  auto logits_of_a = [&] {   // stage 4 (and the prologue); leaves the first fragments and scalars of stage 1 in flight
-    ld_rows(0, 0, 0);
-    dp_start(dpA, lds_f, 0);
-    ld_soft(0);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sA[e] = 0.f;
-#pragma unroll
-    for (int kd = 0; kd < NK; ++kd) {
-      if (kd + 1 < NK) ld_rows((kd + 1) & 1, 0, kd + 1); else ld_rows((kd + 1) & 1, 1, 0);
-      if (kd == NK - 2) dp_start(dpB, lds_f, 1);
-      if (kd == 0) reads_in(R3{}); else if (kd == NK - 2) reads_in(R6{}); else reads_in(R2{});
-      sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], kf[kd], sA, 0, 0, 0);
-      dpA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], vf[kd], dpA, 0, 0, 0);
-      fence();
-    }
-  };
-
-  unsigned cur = 0;   // the stage at hand
-  auto tile = [&](int i0, auto more_tag) {
-    constexpr bool MORE = decltype(more_tag)::value;
-    const unsigned nxt = cur ^ 1u;
-    if (MORE) fetch(nxt * STAGE);   // (every wave left that stage at the barrier below)
-    auto soft = [&](f32x16 &sv, f32x16 &dpv, int q) {   // logits -> P, dP -> dS
-      const int e0 = (q % NK) * EPS;
-#pragma unroll
-      for (int u = 0; u < EPS; ++u) {
-        const float pr = fast_exp2(sv[e0 + u] * c - lsc[q & 1][u]);
-        sv[e0 + u] = pr;
-        dpv[e0 + u] *= pr;
-      }
-    };
-    auto mask = [&](f32x16 &sv, int sub) {
-      const int ib = i0 + 32 * sub;
-      if (ib < jw0 + 31 || (ib + 31 - jw0 >= window && jw0 + 32 > sinks)) hide(sv, hidden_queries(kj, ib, window, sinks), hh);
-    };
-    f32x16 sB;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sB[e] = 0.f;
-    mask(sA, 0);
-#pragma unroll
-    for (int kd = 0; kd < NK; ++kd) {   // stage 1
-      if (kd + 1 < NK) ld_rows((kd + 1) & 1, 1, kd + 1); else ld_cols((kd + 1) & 1, 0, 0);
-      ld_soft(kd + 1);
-      if (kd + 1 < NK) reads_in(R3{}); else reads_in(R5{});
-      sB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], kf[kd], sB, 0, 0, 0);
-      dpB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], vf[kd], dpB, 0, 0, 0);
-      soft(sA, dpA, kd);
-      fence();
-    }
-    bf16x8 pf[2], dsf[2];
-    pf[0] = pack8(sA, 0); pf[1] = pack8(sA, 8); dsf[0] = pack8(dpA, 0); dsf[1] = pack8(dpA, 8);
-    mask(sB, 1);
-#pragma unroll
-    for (int j = 0; j < NK; ++j) {      // stage 2
-      if (j + 1 < NK) ld_cols((j + 1) & 1, 0, j + 1); else ld_cols((j + 1) & 1, 1, 0);
-      if (j + 1 < NK) ld_soft(NK + j + 1);
-      if (j + 1 < NK) reads_in(R5{}); else reads_in(R4{});
-      dv[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], pf[j / ND], dv[j % ND], 0, 0, 0);
-      dk[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[j & 1], dsf[j / ND], dk[j % ND], 0, 0, 0);
-      soft(sB, dpB, NK + j);
-      fence();
-    }
-    pf[0] = pack8(sB, 0); pf[1] = pack8(sB, 8); dsf[0] = pack8(dpB, 0); dsf[1] = pack8(dpB, 8);
-#pragma unroll
-    for (int j = 0; j < NK; ++j) {      // stage 3
-      if (j + 1 < NK) ld_cols((j + 1) & 1, 1, j + 1);
-      if (j + 1 < NK) reads_in(R4{}); else reads_in(R0{});
-      dv[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], pf[j / ND], dv[j % ND], 0, 0, 0);
-      dk[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[j & 1], dsf[j / ND], dk[j % ND], 0, 0, 0);
-      fence();
-    }
-    if (MORE) stash(nxt);
-    at.flip(STAGE);
-    lds_f = reinterpret_cast<const float *>(smem_b + FBASE + nxt * FSTAGE);
-    wait_dma();
-    __syncthreads();
-    cur = nxt;
-    if (MORE) logits_of_a();   // stage 4
-  };
-  if (walk.begin < walk.end) {
-    logits_of_a();
-    int i0 = i_next;
-    for (int it = walk.begin; it + 1 < walk.end; ++it) {
-      tile(i0, std::true_type{});
-      i0 = i_next;
-    }
-    tile(i0, std::false_type{});
-  }
-
-  if (slot < 0) {
-    unsigned char *ew = smem_b + wave * (128 * DH);
-    store_rows<DH>(ew, dk, a.scale, dkb + (long)jw0 * a.ldk, a.ldk, S - jw0, len - jw0, nch, lane);
-    store_rows<DH>(ew + 64 * DH, dv, 1.f, dvb + (long)jw0 * a.ldv, a.ldv, S - jw0, len - jw0, nch, lane);
-    return;
-  }
-  // sums of this piece: a lane's key is a row, its four consecutive columns one store
-  float *out = sums + slot * (2 * BROWS * DH) + (wave * 32 + (lane & 31)) * DH + 4 * hh;
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int e4 = 0; e4 < 4; ++e4) {
-      f32x4 x, y;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) { x[u] = dk[d][4 * e4 + u]; y[u] = dv[d][4 * e4 + u]; }
-      *reinterpret_cast<f32x4 *>(out + 32 * d + 8 * e4) = x;
-      *reinterpret_cast<f32x4 *>(out + BROWS * DH + 32 * d + 8 * e4) = y;
-    }
-}
-
-int columns(const WindowArgs &a) { return a.dh <= 64 ? 64 : 128; }
-
-// (blocks at once: one a CU at 128 columns, two at 64)
-KeyWork work_of(const WindowArgs &a) { return key_work<BROWS>(a, columns(a) == 128 ? kCus : 2 * kCus); }
-
-template <typename K> hipError_t with_lds(K kern, size_t smem) {   // (per device and kernel; beyond 64 KB it has to be asked for)
-  return smem <= 64 * 1024 ? hipSuccess
-                           : hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-}
 
 // Blocks of the same weight go head after head; those of a window that most of the sequence fits in are as uneven as a causal
 // mask's and go by weight.
@@ -656,25 +368,14 @@ template <int DH> hipError_t fwd_launch(const WindowArgs &a, hipStream_t s) {
 }
 
 template <int DH> hipError_t bwd_launch(const WindowArgs &a, hipStream_t s) {
-  const int tiles = (a.S + BROWS - 1) / BROWS, blocks_q = tiles * a.nq * a.B;
-  constexpr size_t smem_q = 2 * 2 * (size_t)BKV * DH * sizeof(bf16);
-  constexpr size_t smem_k = 2 * (2 * (size_t)BKV * DH * sizeof(bf16) + 2 * BKV * sizeof(float));
-  const KeyWork w = work_of(a);
-  hipError_t e = with_lds(window_dkv_kernel<DH>, smem_k);
-  if (e != hipSuccess) return e;
+  const int tiles = (a.S + BROWS - 1) / BROWS, blocks = tiles * a.nq * a.B;
+  constexpr size_t smem = 2 * 2 * (size_t)BKV * DH * sizeof(bf16);
   // dQ first: it leaves the row dots <dO_i, O_i> in the workspace
-  const RowOrder ro = order_of<2>(a, blocks_q, tiles, DH);
-  if (ro.own > 0) hipLaunchKernelGGL((window_dq_kernel<DH, true>), dim3(blocks_q), dim3(256), smem_q, s, a, ro);
-  else hipLaunchKernelGGL((window_dq_kernel<DH, false>), dim3(blocks_q), dim3(256), smem_q, s, a, ro);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  float *sums = (float *)((char *)a.ws + dots_bytes(a));
-  const int heads = a.B * a.nk;
-  hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3((unsigned)(heads * pieces_of(w))), dim3(256), smem_k, s, a, w, a.ws, sums);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  const int cut = key_blocks_cut(w);
-  if (cut == 0) return hipSuccess;
-  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, BROWS, DH>), dim3(heads * cut * 2 * (BROWS / 32)), dim3(256), 0, s, a, w, sums, cut);
-  return hipGetLastError();
+  const RowOrder ro = order_of<2>(a, blocks, tiles, DH);
+  if (ro.own > 0) hipLaunchKernelGGL((window_dq_kernel<DH, true>), dim3(blocks), dim3(256), smem, s, a, ro);
+  else hipLaunchKernelGGL((window_dq_kernel<DH, false>), dim3(blocks), dim3(256), smem, s, a, ro);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_window_dkv(a, a.ws, (float *)((char *)a.ws + dots_bytes(a)), s);
 }
 
 bool fits(const void *p, long ld, int S) {

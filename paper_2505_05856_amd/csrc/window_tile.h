@@ -25,7 +25,8 @@ __device__ __forceinline__ void hide(f32x16 &v, uint32_t hidden, int hh) {
   const int h = (int)(hidden >> (4 * hh));
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
-    const int m = __builtin_amdgcn_sbfe(h, 8 * (e >> 2) + (e & 3), 1);   // all ones where hidden
+    int m;   // all ones where hidden (written out: the compiler makes a test, a compare and a select of it)
+    asm("v_bfe_i32 %0, %1, %2, 1" : "=v"(m) : "v"(h), "n"(8 * (e >> 2) + (e & 3)));
     v[e] = __int_as_float((m & 0xff800000) | (~m & __float_as_int(v[e])));
   }
 }
