@@ -141,6 +141,16 @@ template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once) {
   KeyWork best{}, w;
   w.key_blocks = (a.S + ROWS - 1) / ROWS;
   w.first = a.sinks > 0 && rest > 0 ? (a.sinks + ROWS - 1) / ROWS : 0;
+  double all = 0;   // items: key block kb has min(tiles left from its own on, in_window) a head, `first` of them the rest as well
+  for (int kb = 0; kb < w.key_blocks; ++kb) {
+    const int left = tiles - kb * (ROWS / BKV);
+    if (left >= in_window) {   // (so had all before it: as many as have that many left)
+      const int n = (left - in_window) / (ROWS / BKV) + 1;
+      all += (double)n * in_window;
+      kb += n - 1;
+    } else all += left;
+  }
+  all = (double)heads * (group * all + (double)w.first * rest);
   double best_time = -1;
   auto consider = [&](int length) {   // of a piece, in items, at most
     w.parts = (walk + length - 1) / length;
@@ -148,8 +158,7 @@ template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once) {
     const size_t slots = slots_of(a, w), best_slots = best_time < 0 ? 0 : slots_of(a, best);
     if (best_time >= 0 && slots > kSlots && slots >= best_slots) return;
     const double near = (walk + w.parts - 1) / w.parts, far = w.far > 0 ? (rest + w.far - 1) / w.far : 0, longest = near > far ? near : far;
-    const double pieces = (double)(heads * pieces_of(w)), rounds = pieces / at_once;
-    const double all = heads * ((double)w.key_blocks * w.parts * near + (double)w.first * w.far * far), mean = all / pieces;
+    const double pieces = (double)(heads * pieces_of(w)), rounds = pieces / at_once, mean = all / pieces;
     const double idle = (double)(long)(rounds + 0.999999) - rounds;
     double time = (all + kStart * pieces) / at_once + idle * (mean + kStart) + 0.5 * (longest - mean);
     if (time < longest + kStart) time = longest + kStart;
