@@ -62,8 +62,7 @@ __device__ __forceinline__ void zero_rows(bf16 *dst, long ld, int r0, int r1, in
 }
 
 inline int columns(const WindowArgs &a) { return a.dh <= 64 ? 64 : 128; }
-// (workgroups at once: one a CU at 128 columns, two at 64)
-inline KeyWork work_of(const WindowArgs &a) { return key_work<BROWS>(a, columns(a) == 128 ? kCus : 2 * kCus); }
+inline KeyWork work_of(const WindowArgs &a) { return key_work<BROWS>(a, kCus); }   // (a workgroup a CU)
 
 }  // namespace
 
