@@ -17,12 +17,8 @@ __global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWor
   constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE, VBASE = 2 * STAGE, FBASE = VBASE + BROWS * DH * 2, FSTAGE = 8 * BKV, ROWB = DH * 2;
 
   const int S = a.S, nch = a.dh / 8, group = a.nq / a.nk;
-  // a head's pieces: the far ones first, then the windows' from the first key block on
-  const int per_head = w.key_blocks * w.parts + w.first * w.far;
-  const int wid = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int head = wid / per_head, id = wid - head * per_head, nfar = w.first * w.far;
-  const int kb = id < nfar ? id / w.far : (id - nfar) / w.parts;
-  const int piece = id < nfar ? w.parts + id % w.far : (id - nfar) % w.parts;
+  const Piece at = piece_at(w, blockIdx.x, a.B * a.nk);
+  const int head = at.head, kb = at.kb, piece = at.piece;
   const int kh = head % a.nk, b = head / a.nk;
   const int len = sample_len(a, b);
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;

@@ -216,10 +216,8 @@ __global__ __launch_bounds__(THREADS, ND <= 2 ? 2 : 1) void window_dkv_f32_kerne
   __shared__ __attribute__((aligned(16))) float qs[FR * Tile<ND>::LD], gs[FR * Tile<ND>::LD];
   __shared__ __attribute__((aligned(16))) float rows[2][FR];   // log-sum-exps (log2 domain) and row dots, negated
   const int S = a.S, group = a.nq / a.nk;
-  const int per_head = w.key_blocks * w.parts + w.first * w.far, wid = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int head = wid / per_head, id = wid - head * per_head, nfar = w.first * w.far;
-  const int kb = id < nfar ? id / w.far : (id - nfar) / w.parts;
-  const int piece = id < nfar ? w.parts + id % w.far : (id - nfar) % w.parts;
+  const Piece at = piece_at(w, blockIdx.x, a.B * a.nk);
+  const int head = at.head, kb = at.kb, piece = at.piece;
   const int kh = head % a.nk, b = head / a.nk, len = sample_len(a, b);
   const int lane = threadIdx.x & 63, hh = lane >> 5;
   const int in_block = (int)(threadIdx.x >> 6) * 32 + (lane & 31), kj = kb * ROWS + in_block;

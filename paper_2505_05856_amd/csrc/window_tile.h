@@ -52,7 +52,8 @@ __device__ __forceinline__ int sample_len(const WindowArgs &a, int b) {
 // How the walks over query tiles (64 queries) are cut.  Key block kb (ROWS keys) of a key head walks, for each query head of its
 // group, the tiles from its own first to the end of its window: `parts` pieces.  Key blocks below `first` hold keys that all
 // later queries see: the rest of the sequence, `far` pieces more.
-struct KeyWork { int key_blocks, parts, first, far; };
+// Key blocks below `full` have a whole window of queries after them, the others a shorter walk.
+struct KeyWork { int key_blocks, parts, first, far, full; };
 
 struct Walk { int t0, nt, begin, end; };   // query tiles t0 .. t0+nt-1 of each head in turn; items begin .. end-1 of that list
 template <int ROWS> __host__ __device__ __forceinline__ Walk walk_of(const KeyWork &w, int kb, int piece, int len, int window, int group) {
@@ -68,6 +69,30 @@ template <int ROWS> __host__ __device__ __forceinline__ Walk walk_of(const KeyWo
   r.begin = i * chunk < n ? i * chunk : n;
   r.end = r.begin + chunk < n ? r.begin + chunk : n;
   return r;
+}
+// Which piece a workgroup takes.  Workgroup i runs on XCD i % 8, and an XCD starts its own in order.  Whole walks come first, a head
+// (its far pieces, then its key blocks) after the other: an XCD gets all of a head's, or where the heads do not go round evenly
+// four in a row, so that those that share queries share an L2.  The shorter walks follow, one by one in falling length: they fill
+// the holes that the last whole ones leave, on every XCD alike.  (Contiguous shares in head order gave one XCD the ends of the
+// sequence alone: 16384 tokens of 4 + 1 heads, window 4096, took 1.2 times as long.)
+struct Piece { int head, kb, piece; };
+__device__ __forceinline__ Piece piece_at(const KeyWork &w, int i, int heads) {
+  const int nfar = w.first * w.far, per_head = nfar + w.full * w.parts, whole = heads * per_head;
+  Piece p;
+  if (i < whole) {
+    const int run = heads % 8 == 0 ? per_head : 4, dealt = whole / (8 * run) * (8 * run);
+    const int at = i < dealt ? i / (8 * run) * (8 * run) + i % 8 * run + i / 8 % run : i;
+    p.head = at / per_head;
+    const int id = at - p.head * per_head;
+    p.kb = id < nfar ? id / w.far : (id - nfar) / w.parts;
+    p.piece = id < nfar ? w.parts + id % w.far : (id - nfar) % w.parts;
+  } else {
+    const int id = i - whole, row = id / heads;
+    p.head = id - row * heads;
+    p.kb = w.full + row / w.parts;
+    p.piece = row % w.parts;
+  }
+  return p;
 }
 // Where a piece's sums go: a slot of the workspace (two [ROWS][DH] arrays), or -1: it is its block's only one, the result itself.
 // The slots of a block's window, and those of the rest, follow each other.
@@ -128,40 +153,43 @@ int key_blocks_cut(const KeyWork &w) { return w.parts > 1 ? w.key_blocks : w.fir
 long pieces_of(const KeyWork &w) { return (long)w.key_blocks * w.parts + (long)w.first * w.far; }
 
 // The cut with the smallest estimated time, in items (64 queries of a head).  `at_once` pieces run side by side, each as long as
-// its items and kStart more (its keys, the pipeline's fill, its results); the launch ends a part of a piece later than work evenly
-// spread would, the more so the emptier its last round is and the longer its longest piece.  A slot is written and read once
-// more (two [128][128] arrays: about a 40th of an item of the whole chip's time), and adding up is a launch.  More than kSlots
-// slots of workspace are taken only where no cut does with fewer.
+// its items and kStart more (its keys, the pipeline's fill, its results).  The whole walks take full rounds; what their last round
+// leaves free goes to the shorter ones, and where there are more of those than free places the longest of the rest comes on top.
+// A slot is written and read once more (two [128][128] arrays: about a 40th of an item of the whole chip's time), and adding up is
+// a launch.  More than kSlots slots of workspace are taken only where no cut does with fewer.
 template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once) {
   constexpr double kStart = 3, kSlot = 0.025, kLaunch = 2;
   constexpr size_t kSlots = 4096;
+  constexpr int R = ROWS / BKV;
   const int group = a.nq / a.nk, tiles = (a.S + BKV - 1) / BKV, in_window = (ROWS + a.window - 2) / BKV + 1;   // (as walk_of has them)
   const int walk = group * (tiles < in_window ? tiles : in_window), rest = group * (tiles > in_window ? tiles - in_window : 0);
-  const long heads = (long)a.B * a.nk;
+  const double heads = (double)a.B * a.nk;
   KeyWork best{}, w;
   w.key_blocks = (a.S + ROWS - 1) / ROWS;
   w.first = a.sinks > 0 && rest > 0 ? (a.sinks + ROWS - 1) / ROWS : 0;
-  double all = 0;   // items: key block kb has min(tiles left from its own on, in_window) a head, `first` of them the rest as well
-  for (int kb = 0; kb < w.key_blocks; ++kb) {
-    const int left = tiles - kb * (ROWS / BKV);
-    if (left >= in_window) {   // (so had all before it: as many as have that many left)
-      const int n = (left - in_window) / (ROWS / BKV) + 1;
-      all += (double)n * in_window;
-      kb += n - 1;
-    } else all += left;
-  }
-  all = (double)heads * (group * all + (double)w.first * rest);
+  w.full = tiles >= in_window ? (tiles - in_window) / R + 1 : 0;
+  if (w.full > w.key_blocks) w.full = w.key_blocks;
+  const double n_short = w.key_blocks - w.full;   // (tiles left from their own on: an arithmetic series)
+  const double whole_items = heads * ((double)w.full * walk + (double)w.first * rest);
+  const double short_items = heads * group * n_short * (tiles - R * 0.5 * (w.full + w.key_blocks - 1));
   double best_time = -1;
   auto consider = [&](int length) {   // of a piece, in items, at most
     w.parts = (walk + length - 1) / length;
     w.far = w.first > 0 ? (rest + length - 1) / length : 0;
     const size_t slots = slots_of(a, w), best_slots = best_time < 0 ? 0 : slots_of(a, best);
     if (best_time >= 0 && slots > kSlots && slots >= best_slots) return;
-    const double near = (walk + w.parts - 1) / w.parts, far = w.far > 0 ? (rest + w.far - 1) / w.far : 0, longest = near > far ? near : far;
-    const double pieces = (double)(heads * pieces_of(w)), rounds = pieces / at_once, mean = all / pieces;
-    const double idle = (double)(long)(rounds + 0.999999) - rounds;
-    double time = (all + kStart * pieces) / at_once + idle * (mean + kStart) + 0.5 * (longest - mean);
-    if (time < longest + kStart) time = longest + kStart;
+    const double near = (walk + w.parts - 1) / w.parts + kStart, far = w.far > 0 ? (rest + w.far - 1) / w.far + kStart : 0;
+    const double longest = near > far ? near : far;
+    const double whole = heads * ((double)w.full * w.parts + (double)w.first * w.far), shorts = heads * n_short * w.parts;
+    const double rounds = (double)(long)(whole / at_once), left = whole - rounds * at_once;
+    const double mean = whole > 0 ? whole_items / whole + kStart : 0;
+    double time = (left > 0 ? rounds + 1 : rounds) * mean;
+    const double places = left > 0 ? at_once - left : 0;
+    if (shorts > places) time += near * (1 - places / shorts);
+    if (whole > 0) time += 0.5 * (longest - mean);
+    const double even = (whole_items + short_items + kStart * (whole + shorts)) / at_once + 0.1 * near;
+    if (time < even) time = even;
+    if (time < longest) time = longest;
     time += (double)slots * kSlot + (slots > 0 ? kLaunch : 0);
     if (best_time < 0 || time < best_time || best_slots > kSlots) { best = w; best_time = time; }
   };
