@@ -16,6 +16,8 @@
 
 #include <type_traits>
 
+#include <type_traits>
+
 namespace dp {
 
 namespace {
@@ -271,81 +273,59 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
   wait_dma();
   __syncthreads();
 
-  // the pipeline over the two 32-key sub-tiles A and B of a tile, as in the full attention's dQ kernel
-  constexpr int EPS = 16 / NK;
-  bf16x8 fx[2], fy[2];
-  auto ld_rows = [&](int slot, int sub, int kd) {   // K and V along the rows: operands of S and dP
-    fx[slot] = at.rows(0u, sub * 32, kd);
-    fy[slot] = at.rows(TILE, sub * 32, kd);
-  };
-  auto ld_cols = [&](int slot, int sub, int j) {    // K down the rows: operand of dQ
-    fx[slot] = at.cols(0u, sub * 32 + (j / ND) * 16, j % ND);
-  };
+  constexpr int AHEAD = 3, RING = 4;
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-  f32x16 sA, dpA;
-  auto logits_of_a = [&] {
-    ld_rows(0, 0, 0);
+  // dS of the 32 keys from jb on (sub-tile `sub` of the tile at hand), and what they add to dQ
+  auto block = [&](auto sub_tag, int jb) {
+    constexpr int sub = decltype(sub_tag)::value;
+    bf16x8 fx[RING], fy[RING];
+    auto ld_rows = [&](int i) {   // K and V along the rows: operands of S and dP
+      if (i >= NK) return;
+      fx[i % RING] = at.rows(0u, sub * 32, i);
+      fy[i % RING] = at.rows(TILE, sub * 32, i);
+    };
+    auto ld_cols = [&](int i) {   // K down the rows: operand of dQ
+      if (i < NK) fx[i % RING] = at.cols(0u, sub * 32 + (i / ND) * 16, i % ND);
+    };
+    f32x16 s, dp;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) { sA[e] = 0.f; dpA[e] = 0.f; }
+    for (int i = 0; i < AHEAD; ++i) ld_rows(i);
 #pragma unroll
-    for (int kd = 0; kd < NK; ++kd) {
-      if (kd + 1 < NK) ld_rows((kd + 1) & 1, 0, kd + 1); else ld_rows((kd + 1) & 1, 1, 0);
-      sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], qf[kd], sA, 0, 0, 0);
-      dpA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], gf[kd], dpA, 0, 0, 0);
+    for (int e = 0; e < 16; ++e) { s[e] = 0.f; dp[e] = -dq_i; }   // (dP starts at -D)
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      ld_rows(i + AHEAD);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[i % RING], qf[i], s, 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[i % RING], gf[i], dp, 0, 0, 0);
+      fence();
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ld_cols(i);
+    if (jb + 31 > iw0 || (iw0 + 31 - jb >= window && jb + 32 > sinks)) hide(s, hidden_keys(qi, jb, window, sinks), hh);
+    bf16x8 dsf[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int e = 8 * h; e < 8 * h + 8; ++e) dp[e] *= fast_exp2(s[e] * c - lq);
+      dsf[h] = pack8(dp, 8 * h);
+    }
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      ld_cols(i + AHEAD);
+      dq[i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[i % RING], dsf[i / ND], dq[i % ND], 0, 0, 0);
       fence();
     }
   };
-  logits_of_a();
-
+  // (nothing to do where every key comes after the queries or before their windows, past the first keys)
+  auto seen = [&](int jb) { return jb <= iw0 + 31 && (iw0 - (jb + 31) < window || jb < sinks); };
   for (int t = 0; t < kt.n; ++t) {
     const int j0 = kt.first_key(t);
     if (t + 1 < kt.n) fetch(t + 1, (unsigned)((t & 1) ^ 1) * STAGE);   // (every wave left that stage at the barrier below)
-    {
-      auto mask = [&](f32x16 &sv, int sub) {
-        const int jb = j0 + 32 * sub;
-        if (jb + 31 > iw0 || (iw0 + 31 - jb >= window && jb + 32 > sinks)) hide(sv, hidden_keys(qi, jb, window, sinks), hh);
-      };
-      auto soft = [&](f32x16 &sv, f32x16 &dpv, int e0) {   // logits -> P, dP -> dS
-#pragma unroll
-        for (int u = 0; u < EPS; ++u) {
-          const int e = e0 + u;
-          dpv[e] = fast_exp2(sv[e] * c - lq) * (dpv[e] - dq_i);
-        }
-      };
-      f32x16 sB, dpB;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) { sB[e] = 0.f; dpB[e] = 0.f; }
-      mask(sA, 0);
-#pragma unroll
-      for (int kd = 0; kd < NK; ++kd) {   // stage 1
-        if (kd + 1 < NK) ld_rows((kd + 1) & 1, 1, kd + 1); else ld_cols((kd + 1) & 1, 0, 0);
-        sB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[kd & 1], qf[kd], sB, 0, 0, 0);
-        dpB = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[kd & 1], gf[kd], dpB, 0, 0, 0);
-        soft(sA, dpA, kd * EPS);
-        fence();
-      }
-      bf16x8 dsf[2];
-      dsf[0] = pack8(dpA, 0); dsf[1] = pack8(dpA, 8);
-      mask(sB, 1);
-#pragma unroll
-      for (int j = 0; j < NK; ++j) {      // stage 2
-        if (j + 1 < NK) ld_cols((j + 1) & 1, 0, j + 1); else ld_cols((j + 1) & 1, 1, 0);
-        dq[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], dsf[j / ND], dq[j % ND], 0, 0, 0);
-        soft(sB, dpB, j * EPS);
-        fence();
-      }
-      dsf[0] = pack8(dpB, 0); dsf[1] = pack8(dpB, 8);
-#pragma unroll
-      for (int j = 0; j < NK; ++j) {      // stage 3
-        if (j + 1 < NK) ld_cols((j + 1) & 1, 1, j + 1);
-        dq[j % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[j & 1], dsf[j / ND], dq[j % ND], 0, 0, 0);
-        fence();
-      }
-    }
+    if (seen(j0)) block(std::integral_constant<int, 0>{}, j0);
+    if (seen(j0 + 32)) block(std::integral_constant<int, 1>{}, j0 + 32);
     at.flip(STAGE);
     wait_dma();
     __syncthreads();
-    if (t + 1 < kt.n) logits_of_a();   // stage 4
   }
 
   store_rows<DH>(smem_b + wave * (64 * DH), dq, a.scale, dqb + (long)iw0 * a.ldq, a.ldq, S - iw0, len - iw0, nch, lane);
