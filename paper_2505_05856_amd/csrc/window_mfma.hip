@@ -16,13 +16,159 @@
 
 #include <type_traits>
 
-#include <type_traits>
-
 namespace dp {
 
 namespace {
 
-// ------------------------------------------------------------------ forward
+// ------------------------------------------------------------------ forward, many blocks and short windows
+// Tiles of 32 keys, one after the other, and none that the window or the order of the tokens hides from all of a wave's queries: of
+// a window of 512 the pipeline below takes 704 keys a query, this 560.  What hides the softmax are two (64 columns: three) more
+// waves on the SIMD, which half as much LDS leaves room for; where a CU has fewer blocks than that, or the window is long, the
+// pipeline is ahead.  The pipeline and this, us (heads of 128 with a quarter as many key heads):
+//   blocks of 128 queries       window 64       256           1024          4096
+//   256 (4096 tokens, 8 heads)  11.1, 11.1      14.5, 15.5    27.0, 30.8    72.9, 86.9
+//   1024 (2 x 4096, 16)         27.0, 24.6      36.9, 38.0    76.7, 81.9    143, 163
+//   2048 (4 x 2048, 32)         48.6, 42.5      67.4, 59.1    127, 122      151, 160
+//   4096 (8 x 2048, 32)         105, 94.6       144, 125      255, 242      304, 303
+// Heads of 64:  1024 blocks     15.8, 14.9      24.4, 20.8    50.9, 47.3    85.3, 89.4
+//   4096                        52.3, 41.3      74.5, 64.3    141, 139      173, 174
+constexpr int KEYS = 32;
+bool by_blocks(const WindowArgs &a, int blocks) { return blocks > 2 * kCus && a.window <= 512; }
+template <int DH>
+__global__ __launch_bounds__(256, DH == 64 ? 4 : 3) void window_fwd_blocks_kernel(WindowArgs a, RowOrder ro) {
+  constexpr int ND = DH / 32, NK = DH / 16;
+  // LDS, in bytes: [stage 0: K, V][stage 1: K, V]
+  constexpr unsigned TILE = KEYS * DH * 2, STAGE = 2 * TILE;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
+
+  const int S = a.S, nqt = (S + BROWS - 1) / BROWS, nch = a.dh / 8;
+  int rank, head;
+  if (ro.own > 0) row_tile<true>(ro, blockIdx.x, gridDim.x, nqt, &rank, &head);
+  else row_tile<false>(ro, blockIdx.x, gridDim.x, nqt, &rank, &head);
+  const int q0 = (nqt - 1 - rank) * BROWS;   // (late tiles are the heavy ones)
+  const int h = head % a.nq, b = head / a.nq, kh = h / (a.nq / a.nk);
+  const int len = sample_len(a, b);
+  const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int iw0 = q0 + wave * 32, qi = iw0 + (lane & 31);
+  bf16 *ob = (bf16 *)a.o + (long)b * S * a.ldo + (long)h * a.dh;
+  float *lb = a.lse + ((long)b * a.nq + h) * S;
+  if (q0 >= len) {
+    const int r1 = min(q0 + BROWS, S);
+    if (a.o != nullptr) zero_rows(ob, a.ldo, q0, r1, nch);
+    if (a.lse != nullptr && q0 + tid < r1) lb[q0 + tid] = -INFINITY;
+    return;
+  }
+  const bf16 *qb = (const bf16 *)a.q + (long)b * S * a.ldq + (long)h * a.dh;
+  const char *kb = uniform_ptr((const char *)((const bf16 *)a.k + (long)b * S * a.ldk + (long)kh * a.dh));
+  const char *vb = uniform_ptr((const char *)((const bf16 *)a.v + (long)b * S * a.ldv + (long)kh * a.dh));
+  const unsigned ldkb = (unsigned)a.ldk * 2u, ldvb = (unsigned)a.ldv * 2u;
+  const float c = a.scale * kLog2e;
+  const int window = a.window, sinks = a.sinks;
+  const KeyTiles<KEYS, BROWS> kt(q0, len, window, sinks);
+  auto fetch = [&](int t, unsigned buf) {
+    const int j0 = kt.first_key(t);
+    dma_tile<DH, KEYS, 4>(buf, kb, ldkb, j0, len, nch, wave, lane);
+    dma_tile<DH, KEYS, 4>(buf + TILE, vb, ldvb, j0, len, nch, wave, lane);
+  };
+  fetch(0, 0u);
+
+  bf16x8 qf[NK];
+  const bf16 *qrow = qb + (long)min(qi, len - 1) * a.ldq;   // (a query past the end reads the last row, and nothing of it is stored)
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd) qf[kd] = row_frag(qrow, kd, hh, a.dh);
+
+  f32x16 acc[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
+  float m = -1e30f, l = 0.f;   // m: reference point of the exponents (log2 domain)
+
+  BothAddr<DH> at;
+  at.init(lane);
+  wait_dma();
+#pragma unroll
+  for (int kd = 0; kd < NK; ++kd) asm volatile("" ::"v"(qf[kd]));   // (the fragments are waited for here, not in the tile loop)
+  __syncthreads();
+
+  constexpr int AHEAD = 3, RING = 4;
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  // keys jb .. jb+31, a tile
+  auto block = [&](auto stage_tag, int jb) {
+    constexpr unsigned base = decltype(stage_tag)::value * STAGE;
+    bf16x8 fx[RING];
+    auto ld_rows = [&](int i) { if (i < NK) fx[i % RING] = at.rows(base, 0, i); };
+    auto ld_cols = [&](int i) { if (i < NK) fx[i % RING] = at.cols(base + TILE, (i / ND) * 16, i % ND); };
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ld_rows(i);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      ld_rows(i + AHEAD);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[i % RING], qf[i], s, 0, 0, 0);
+      fence();
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ld_cols(i);
+    if (jb + 31 > iw0 || (iw0 + 31 - jb >= window && jb + 32 > sinks)) hide(s, hidden_keys(qi, jb, window, sinks), hh);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    const float m_new = fmaxf(m, halves_max(mx) * c);
+    constexpr float kLag = 8.f;   // (the reference point follows the maximum only when it is left behind by a factor of 2^8)
+    if (__builtin_amdgcn_ballot_w64(m_new > m + kLag) != 0) {
+      const float alpha = fast_exp2(m - m_new);
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+      m = m_new;
+    }
+    bf16x8 pf[2];
+    float ps = 0.f;
+#pragma unroll
+    for (int h2 = 0; h2 < 2; ++h2) {
+#pragma unroll
+      for (int e = 8 * h2; e < 8 * h2 + 8; ++e) {
+        s[e] = fast_exp2(__builtin_fmaf(s[e], c, -m));
+        ps += s[e];
+      }
+      pf[h2] = pack8(s, 8 * h2);
+    }
+    l += ps;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      ld_cols(i + AHEAD);
+      acc[i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[i % RING], pf[i / ND], acc[i % ND], 0, 0, 0);
+      fence();
+    }
+  };
+  // (nothing to do where every key comes after the queries or before their windows, past the first keys)
+  auto seen = [&](int jb) { return jb <= iw0 + 31 && (iw0 - (jb + 31) < window || jb < sinks); };
+  auto tile = [&](int t, auto stage_tag) {
+    constexpr int stage = decltype(stage_tag)::value;
+    const int j0 = kt.first_key(t);
+    if (t + 1 < kt.n) fetch(t + 1, (unsigned)(stage ^ 1) * STAGE);   // (every wave left that stage at the barrier below)
+    if (seen(j0)) block(stage_tag, j0);
+    wait_dma();
+    __syncthreads();
+  };
+  for (int t = 0; t < kt.n; t += 2) {
+    tile(t, std::integral_constant<int, 0>{});
+    if (t + 1 < kt.n) tile(t + 1, std::integral_constant<int, 1>{});
+  }
+
+  l += __shfl_xor(l, 32, 64);
+  if (a.lse != nullptr && hh == 0 && qi < S) lb[qi] = qi < len ? (m + __log2f(l)) * kLn2 : -INFINITY;
+  if (a.o == nullptr) return;
+  store_rows<DH>(smem_b + wave * (64 * DH), acc, 1.0f / l, ob + (long)iw0 * a.ldo, a.ldo, S - iw0, len - iw0, nch, lane);
+}
+
+// ------------------------------------------------------------------ forward, otherwise
 // The pipeline of a tile is the full attention's (attn_mfma.hip): the logits of tile t+1 are taken beside the softmax of tile t.
 template <int DH, bool ORDERED>
 __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void window_fwd_kernel(WindowArgs a, RowOrder ro) {
@@ -340,6 +486,12 @@ template <int PER_CU> RowOrder order_of(const WindowArgs &a, int blocks, int til
 
 template <int DH> hipError_t fwd_launch(const WindowArgs &a, hipStream_t s) {
   const int tiles = (a.S + BROWS - 1) / BROWS, blocks = tiles * a.nq * a.B;
+  if (by_blocks(a, blocks)) {
+    constexpr size_t smem = 2 * 2 * (size_t)KEYS * DH * sizeof(bf16);
+    const RowOrder ro = order_of<DH == 64 ? 4 : 3>(a, blocks, tiles, DH);
+    hipLaunchKernelGGL((window_fwd_blocks_kernel<DH>), dim3(blocks), dim3(256), smem, s, a, ro);
+    return hipGetLastError();
+  }
   constexpr size_t smem = 2 * 2 * (size_t)BKV * DH * sizeof(bf16);
   const RowOrder ro = order_of<DH == 64 ? 3 : 2>(a, blocks, tiles, DH);
   if (ro.own > 0) hipLaunchKernelGGL((window_fwd_kernel<DH, true>), dim3(blocks), dim3(256), smem, s, a, ro);

@@ -175,6 +175,22 @@ def test_long(dt, S, window, sinks, nq, nk):
 
 
 @gpu
+@pytest.mark.parametrize("Bn,S,nq,nk,dh,window,sinks,lens", [(4, 130, 66, 66, 64, 33, 2, None), (3, 300, 64, 8, 128, 70, 5, [300, 129, 0]), (1, 390, 180, 90, 40, 512, 0, None),
+                                                             (2, 513, 54, 27, 96, 1, 0, [511, 513]), (9, 90, 58, 29, 128, 31, 40, [90, 1, 33, 64, 65, 89, 2, 32, 31])])
+def test_short_windows_of_many_heads(Bn, S, nq, nk, dh, window, sinks, lens):
+    case(Bn, S, nq, nk, dh, window, sinks, lens=lens, packed=lens is not None)
+
+
+@gpu
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("Bn,S,nq,nk,window,sinks,lens", [(1, 1000, 8, 8, 200, 3, None), (2, 700, 8, 4, 100, 130, [700, 333]), (1, 2000, 1, 1, 300, 1, None),
+                                                          (5, 400, 3, 3, 64, 0, None), (8, 300, 2, 1, 300, 0, None)])
+def test_walks_of_keys_dealt_and_cut(Bn, S, nq, nk, window, sinks, lens, dt):
+    """Numbers of key heads that eight does and does not divide, whole and shortened walks, pieces of both."""
+    case(Bn, S, nq, nk, 128 if dt == BF else 64, window, sinks, lens=lens, dt=dt)
+
+
+@gpu
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_gradients_against_differences(dt):
     d = make(1, 40, 2, 1, 64, dt, 5)
