@@ -153,12 +153,12 @@ int key_blocks_cut(const KeyWork &w) { return w.parts > 1 ? w.key_blocks : w.fir
 long pieces_of(const KeyWork &w) { return (long)w.key_blocks * w.parts + (long)w.first * w.far; }
 
 // The cut with the smallest estimated time, in items (64 queries of a head).  `at_once` pieces run side by side, each as long as
-// its items and kStart more (its keys, the pipeline's fill, its results).  The whole walks take full rounds; what their last round
+// its items and `start` more (its keys, the pipeline's fill, its results).  The whole walks take full rounds; what their last round
 // leaves free goes to the shorter ones, and where there are more of those than free places the longest of the rest comes on top.
-// A slot is written and read once more (two [128][128] arrays: about a 40th of an item of the whole chip's time), and adding up is
-// a launch.  More than kSlots slots of workspace are taken only where no cut does with fewer.
-template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once) {
-  constexpr double kStart = 3, kSlot = 0.025, kLaunch = 2;
+// A slot is written and read once more, and adding up is a launch: `slot` and `launch`.  More than kSlots slots of workspace are
+// taken only where no cut does with fewer.
+struct Costs { double start, slot, launch; };   // in items
+template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once, const Costs &cost) {
   constexpr size_t kSlots = 4096;
   constexpr int R = ROWS / BKV;
   const int group = a.nq / a.nk, tiles = (a.S + BKV - 1) / BKV, in_window = (ROWS + a.window - 2) / BKV + 1;   // (as walk_of has them)
@@ -178,19 +178,19 @@ template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once) {
     w.far = w.first > 0 ? (rest + length - 1) / length : 0;
     const size_t slots = slots_of(a, w), best_slots = best_time < 0 ? 0 : slots_of(a, best);
     if (best_time >= 0 && slots > kSlots && slots >= best_slots) return;
-    const double near = (walk + w.parts - 1) / w.parts + kStart, far = w.far > 0 ? (rest + w.far - 1) / w.far + kStart : 0;
+    const double near = (walk + w.parts - 1) / w.parts + cost.start, far = w.far > 0 ? (rest + w.far - 1) / w.far + cost.start : 0;
     const double longest = near > far ? near : far;
     const double whole = heads * ((double)w.full * w.parts + (double)w.first * w.far), shorts = heads * n_short * w.parts;
     const double rounds = (double)(long)(whole / at_once), left = whole - rounds * at_once;
-    const double mean = whole > 0 ? whole_items / whole + kStart : 0;
+    const double mean = whole > 0 ? whole_items / whole + cost.start : 0;
     double time = (left > 0 ? rounds + 1 : rounds) * mean;
     const double places = left > 0 ? at_once - left : 0;
     if (shorts > places) time += near * (1 - places / shorts);
     if (whole > 0) time += 0.5 * (longest - mean);
-    const double even = (whole_items + short_items + kStart * (whole + shorts)) / at_once + 0.1 * near;
+    const double even = (whole_items + short_items + cost.start * (whole + shorts)) / at_once + 0.1 * near;
     if (time < even) time = even;
     if (time < longest) time = longest;
-    time += (double)slots * kSlot + (slots > 0 ? kLaunch : 0);
+    time += (double)slots * cost.slot + (slots > 0 ? cost.launch : 0);
     if (best_time < 0 || time < best_time || best_slots > kSlots) { best = w; best_time = time; }
   };
   consider(walk);
