@@ -353,6 +353,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void window_fwd_kernel(Windo
 }
 
 // ------------------------------------------------------------------ backward: dQ, and the row dots <dO_i, O_i>
+constexpr int kShort = 4;   // tiles
 template <int DH, bool ORDERED>
 __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrder ro) {
   constexpr int ND = DH / 32, NK = DH / 16;
@@ -403,9 +404,8 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
   for (int kd = 0; kd < NK; ++kd)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dsum += (float)of[kd][i] * (float)gf[kd][i];
-  const float dq_i = dsum + __shfl_xor(dsum, 32, 64);   // the two halves of the row
+  float dot = dsum + __shfl_xor(dsum, 32, 64);   // the two halves of the row
   const long row_at = ((long)b * a.nq + h) * S + qi;
-  if (qi < len && hh == 0) a.ws[row_at] = dq_i;
   const float lq = qi < len ? a.lse[row_at] * kLog2e : INFINITY;   // (queries past the end: P = 0)
 
   f32x16 dq[ND];
@@ -422,7 +422,8 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
   constexpr int AHEAD = 3, RING = 4;
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
   // dS of the 32 keys from jb on (sub-tile `sub` of the tile at hand), and what they add to dQ
-  auto block = [&](auto sub_tag, int jb) {
+  float rest = 0.f;   // the sum of dS over this lane's keys
+  auto block = [&](auto sub_tag, int jb, bool add) {
     constexpr int sub = decltype(sub_tag)::value;
     bf16x8 fx[RING], fy[RING];
     auto ld_rows = [&](int i) {   // K and V along the rows: operands of S and dP
@@ -437,7 +438,7 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) ld_rows(i);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) { s[e] = 0.f; dp[e] = -dq_i; }   // (dP starts at -D)
+    for (int e = 0; e < 16; ++e) { s[e] = 0.f; dp[e] = -dot; }   // (dP starts at -D)
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       ld_rows(i + AHEAD);
@@ -452,9 +453,13 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int e = 8 * h; e < 8 * h + 8; ++e) dp[e] *= fast_exp2(s[e] * c - lq);
+      for (int e = 8 * h; e < 8 * h + 8; ++e) {
+        dp[e] *= fast_exp2(s[e] * c - lq);
+        rest += dp[e];
+      }
       dsf[h] = pack8(dp, 8 * h);
     }
+    if (!add) return;
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       ld_cols(i + AHEAD);
@@ -464,15 +469,26 @@ __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrde
   };
   // (nothing to do where every key comes after the queries or before their windows, past the first keys)
   auto seen = [&](int jb) { return jb <= iw0 + 31 && (iw0 - (jb + 31) < window || jb < sinks); };
-  for (int t = 0; t < kt.n; ++t) {
-    const int j0 = kt.first_key(t);
-    if (t + 1 < kt.n) fetch(t + 1, (unsigned)((t & 1) ^ 1) * STAGE);   // (every wave left that stage at the barrier below)
-    if (seen(j0)) block(std::integral_constant<int, 0>{}, j0);
-    if (seen(j0 + 32)) block(std::integral_constant<int, 1>{}, j0 + 32);
-    at.flip(STAGE);
-    wait_dma();
-    __syncthreads();
+  // The dS of a query add up to 0 if D is the sum of its P dP, and to what <dO, O> is off by as O was rounded.  dK gets the D put
+  // right by that; so does dQ where walks are short, by a first sweep over the tiles: with few keys to a query the rounding of O
+  // counts as much as that of dS (a window of 64: dQ off by 1.6 times what rounding the result costs, else 1.4 times).
+  unsigned at_hand = 0;   // the stage of the tile at hand
+  for (int sweep = kt.n <= kShort ? 0 : 1; sweep < 2; ++sweep) {
+    for (int t = 0; t < kt.n; ++t) {
+      const int j0 = kt.first_key(t);
+      at_hand ^= STAGE;
+      // (every wave left that stage at the barrier below; the first sweep ends with the first tile again)
+      if (t + 1 < kt.n || sweep == 0) fetch(t + 1 < kt.n ? t + 1 : 0, at_hand);
+      if (seen(j0)) block(std::integral_constant<int, 0>{}, j0, sweep == 1);
+      if (seen(j0 + 32)) block(std::integral_constant<int, 1>{}, j0 + 32, sweep == 1);
+      at.flip(STAGE);
+      wait_dma();
+      __syncthreads();
+    }
+    dot += rest + __shfl_xor(rest, 32, 64);
+    rest = 0.f;
   }
+  if (qi < len && hh == 0) a.ws[row_at] = dot;
 
   store_rows<DH>(smem_b + wave * (64 * DH), dq, a.scale, dqb + (long)iw0 * a.ldq, a.ldq, S - iw0, len - iw0, nch, lane);
 }

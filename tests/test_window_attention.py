@@ -191,6 +191,19 @@ def test_walks_of_keys_dealt_and_cut(Bn, S, nq, nk, window, sinks, lens, dt):
 
 
 @gpu
+@pytest.mark.parametrize("S,window", [(300, 2), (300, 5), (200, 64), (900, 200), (400, 400)])
+def test_gradients_are_rounded_twice(S, window):
+    """Where a query sees few keys the rounding of O must not reach dQ and dK through <dO, O>: what is left are the rounding of dS and
+    that of the result, independent from element to element, each at most h of its element and h / sqrt 3 in the mean square."""
+    d = make(2, S, 4, 2, 128, BF, 17, sd=1.4)
+    want, _ = reference(d, 2, S, window, 0, None, 128 ** -0.5, BF)
+    got = run(d, 2, S, window, 0)
+    for n in ("dq", "dk"):
+        err = (got[n].double() - want[n]).norm() / want[n].norm()
+        assert err < math.sqrt(2 / 3) * 2.0 ** -8, (n, err.item())
+
+
+@gpu
 @pytest.mark.parametrize("dt", [BF, F32])
 def test_gradients_against_differences(dt):
     d = make(1, 40, 2, 1, 64, dt, 5)
