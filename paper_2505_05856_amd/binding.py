@@ -586,18 +586,19 @@ def _bad(text: str):
 
 def _heads(name, t, dt, device, rows=None, heads=None, dim=None):
     """[rows, heads, head_dim] with whole heads side by side (a column block of a packed tensor is one): its row stride.  What the
-    library cannot see from a pointer is checked here: element type, shape, the inner strides, the device."""
-    if t.dim() != 3 or t.dtype != dt:
-        _bad(f"{name}: a tensor [rows, heads, head_dim] of {dt} is expected, got {tuple(t.shape)} of {t.dtype}")
-    n, h, d = t.shape
+    library cannot see from a pointer is checked here: element type, shape, the inner strides, the device (its number)."""
+    shape = t.shape
+    if len(shape) != 3 or t.dtype is not dt:
+        _bad(f"{name}: a tensor [rows, heads, head_dim] of {dt} is expected, got {tuple(shape)} of {t.dtype}")
+    n, h, d = shape
     if (rows is not None and n != rows) or (heads is not None and h != heads) or (dim is not None and d != dim):
-        _bad(f"{name}: shape {tuple(t.shape)} does not match ({rows}, {heads}, {dim})")
-    s = t.stride()
-    if (d > 1 and s[2] != 1) or (h > 1 and s[1] != d):
-        _bad(f"{name}: the heads of a row must lie side by side (strides {s})")
-    if t.device != device:
-        _bad(f"{name}: on {t.device}, the call is for {device}")
-    return s[0] if n > 1 else max(s[0], h * d)
+        _bad(f"{name}: shape {tuple(shape)} does not match ({rows}, {heads}, {dim})")
+    row, head, inner = t.stride()
+    if (inner != 1 and d > 1) or (head != d and h > 1):
+        _bad(f"{name}: the heads of a row must lie side by side (strides {t.stride()})")
+    if t.get_device() != device:
+        _bad(f"{name}: on {t.device}, the call is for device {device}")
+    return row if n > 1 else max(row, h * d)
 
 
 def _vector(name, t, dt, device, n, optional=True):
@@ -605,27 +606,27 @@ def _vector(name, t, dt, device, n, optional=True):
         if not optional:
             _bad(f"{name} is missing")
         return
-    if t.numel() != n or t.dtype != dt or not t.is_contiguous() or t.device != device:
-        _bad(f"{name}: {n} contiguous elements of {dt} on {device} are expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.numel() != n or t.dtype is not dt or t.get_device() != device or not t.is_contiguous():
+        _bad(f"{name}: {n} contiguous elements of {dt} on device {device} are expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
 def _call_device(t):
-    """The device of a call's tensors, which must be the current one (kernels go to the current device's stream)."""
+    """The number of the device of a call's tensors, which must be the current one (kernels go to the current device's stream)."""
     import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         _bad(f"tensors on {t.device}: the operators work on the current device")
-    return t.device
+    return t.get_device()
 
 
 def _rotary_shape(q, k, q_out, k_out, q_gain, k_gain, inv_freq, positions, seq, interleaved, eps, scale):
     import torch
-    dev, (T, nq, dh) = _call_device(q), q.shape if q.dim() == 3 else (-1, -1, -1)
-    lq = _heads("q", q, q.dtype, dev)
-    lk = _heads("k", k, q.dtype, dev, T, None, dh)
+    dev, dt, (T, nq, dh) = _call_device(q), q.dtype, q.shape if q.dim() == 3 else (-1, -1, -1)
+    lq = _heads("q", q, dt, dev)
+    lk = _heads("k", k, dt, dev, T, None, dh)
     nk = k.shape[1]
-    lqo, lko = _heads("q_out", q_out, q.dtype, dev, T, nq, dh), _heads("k_out", k_out, q.dtype, dev, T, nk, dh)
-    _vector("q_gain", q_gain, q.dtype, dev, dh)
-    _vector("k_gain", k_gain, q.dtype, dev, dh)
+    lqo, lko = _heads("q_out", q_out, dt, dev, T, nq, dh), _heads("k_out", k_out, dt, dev, T, nk, dh)
+    _vector("q_gain", q_gain, dt, dev, dh)
+    _vector("k_gain", k_gain, dt, dev, dh)
     n = 0 if inv_freq is None else inv_freq.numel()
     _vector("inv_freq", inv_freq, torch.float32, dev, n)
     _vector("positions", positions, torch.int32, dev, T)
@@ -649,13 +650,13 @@ def op_qk_rotary_bwd(dq_out, dk_out, q, k, q_gain, k_gain, inv_freq, dq, dk, dq_
                      scale=1.0, positions=None, stream=None):
     """The gradients of q, k (rows as dq, dk lie) and of the gains.  q and k may be None where there is no gain."""
     shape = _rotary_shape(dq, dk, dq_out, dk_out, q_gain, k_gain, inv_freq, positions, seq, interleaved, eps, scale)
-    dev = dq.device
+    dev = dq.get_device()
     for name, x, of, ld, gain, dg in (("q", q, dq, shape.ldq_in, q_gain, dq_gain), ("k", k, dk, shape.ldk_in, k_gain, dk_gain)):
         if x is not None and _heads(name, x, dq.dtype, dev, *of.shape) != ld:
             _bad(f"{name} and its gradient must have the same row stride")
         if gain is not None:
             _vector(f"d{name}_gain", dg, dq.dtype, dev, of.shape[2], optional=False)
-    if (q_gain is not None or k_gain is not None) and (ws is None or ws.device != dev or ws.numel() * ws.element_size() <
+    if (q_gain is not None or k_gain is not None) and (ws is None or ws.get_device() != dev or ws.numel() * ws.element_size() <
                                                        op_qk_rotary_workspace_bytes(*dq.shape[:2], dk.shape[1], dq.shape[2])):
         _bad("the workspace is smaller than op_qk_rotary_workspace_bytes")
     _check(lib().dp_op_qk_rotary_bwd(_dt(dq), C.byref(shape), _ptr(dq_out), _ptr(dk_out), _ptr(q), _ptr(k), _ptr(q_gain), _ptr(k_gain),
@@ -663,22 +664,18 @@ def op_qk_rotary_bwd(dq_out, dk_out, q, k, q_gain, k_gain, inv_freq, dq, dk, dq_
                                      _stream_ptr(stream)))
 
 
-def _window_shape(q, k, v, o, seq, window, sinks, scale, lens):
+def _window_shape(q, k, v, o, lse, seq, window, sinks, scale, lens):
     import torch
-    dev, (T, nq, dh) = _call_device(q), q.shape if q.dim() == 3 else (-1, -1, -1)
-    lq, lk = _heads("q", q, q.dtype, dev), _heads("k", k, q.dtype, dev, T, None, dh)
+    dev, dt, (T, nq, dh) = _call_device(q), q.dtype, q.shape if q.dim() == 3 else (-1, -1, -1)
+    lq, lk = _heads("q", q, dt, dev), _heads("k", k, dt, dev, T, None, dh)
     nk = k.shape[1]
-    lv = _heads("v", v, q.dtype, dev, T, nk, dh)
-    lo = nq * dh if o is None else _heads("o", o, q.dtype, dev, T, nq, dh)
+    lv = _heads("v", v, dt, dev, T, nk, dh)
+    lo = nq * dh if o is None else _heads("o", o, dt, dev, T, nq, dh)
     if seq < 1 or T % seq:
         _bad(f"{T} rows are no whole samples of {seq}")
     _vector("lens", lens, torch.int32, dev, T // seq)
+    _vector("lse", lse, torch.float32, dev, T * nq)
     return WindowAttention(T // seq, seq, nq, nk, dh, window, sinks, dh ** -0.5 if scale is None else scale, lq, lk, lv, lo)
-
-
-def _row_sums(lse, q, seq):
-    import torch
-    _vector("lse", lse, torch.float32, q.device, q.shape[0] * q.shape[1])
 
 
 def op_window_attention_workspace_bytes(q, k, seq, window, sinks) -> int:
@@ -692,22 +689,21 @@ def op_window_attention_workspace_bytes(q, k, seq, window, sinks) -> int:
 def op_window_attention_fwd(q, k, v, seq, window, sinks, o, lse, lens=None, scale=None, stream=None):
     """o, lse of causal attention over the `window` newest keys and the first `sinks` (scale: head_dim ** -0.5).  q and o are
     [rows, q_heads, head_dim], k and v [rows, kv_heads, head_dim], rows in samples of `seq`; views of a packed projection will do."""
-    shape = _window_shape(q, k, v, o, seq, window, sinks, scale, lens)
-    _row_sums(lse, q, seq)
+    shape = _window_shape(q, k, v, o, lse, seq, window, sinks, scale, lens)
     _check(lib().dp_op_window_attention_fwd(_dt(q), C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o), _ptr(lse),
                                             _stream_ptr(stream)))
 
 
 def op_window_attention_bwd(q, k, v, o, lse, d_o, seq, window, sinks, dq, dk, dv, ws, lens=None, scale=None, stream=None):
     """dq, dk, dv, which lie as q, k, v do (the same row strides); d_o as o."""
-    shape = _window_shape(q, k, v, o, seq, window, sinks, scale, lens)
-    _row_sums(lse, q, seq)
+    shape = _window_shape(q, k, v, o, lse, seq, window, sinks, scale, lens)
     if lse is None or o is None:
         _bad("the backward needs o and lse")
-    for name, t, of, ld in (("d_o", d_o, o, shape.ldo), ("dq", dq, q, shape.ldq), ("dk", dk, k, shape.ldk), ("dv", dv, v, shape.ldv)):
-        if _heads(name, t, q.dtype, q.device, *of.shape) != ld:
+    dev, dt, T, nq, nk, dh = q.get_device(), q.dtype, q.shape[0], shape.q_heads, shape.kv_heads, shape.head_dim
+    for name, t, n, ld in (("d_o", d_o, nq, shape.ldo), ("dq", dq, nq, shape.ldq), ("dk", dk, nk, shape.ldk), ("dv", dv, nk, shape.ldv)):
+        if _heads(name, t, dt, dev, T, n, dh) != ld:
             _bad(f"{name} must have the row stride of what it belongs to")
-    if ws is None or ws.device != q.device or ws.numel() * ws.element_size() < lib().dp_op_window_attention_workspace_bytes(_dt(q), C.byref(shape)):
+    if ws is None or ws.get_device() != dev or ws.numel() * ws.element_size() < lib().dp_op_window_attention_workspace_bytes(_dt(q), C.byref(shape)):
         _bad("the workspace is smaller than op_window_attention_workspace_bytes")
     _check(lib().dp_op_window_attention_bwd(_dt(q), C.byref(shape), _ptr(q), _ptr(k), _ptr(v), _ptr(lens), _ptr(o), _ptr(lse), _ptr(d_o),
                                             _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), _stream_ptr(stream)))
