@@ -7,21 +7,27 @@ namespace dp {
 namespace {
 
 // ---- tiles whose heads may be narrower than the kernel ---------------------------------------------------
-// request i of those a wave issues for a tile of ROWS rows (as dma_req_both): chunks past the head's `nch` read its first
+// A tile of ROWS rows from row0 on: its first row and how many more there are (a tile past the end: the last row).  Offsets count from
+// the tile's own start, so a sample may span more than 4 GiB.
+struct TileRows { const char *at; int more; };
+__device__ __forceinline__ TileRows tile_rows(const char *src, unsigned ldb, int row0, int nrows) {
+  const int first = min(row0, nrows - 1);
+  return TileRows{src + (long)first * ldb, nrows - 1 - first};
+}
+// request i of those a wave issues for it (as dma_req_both): chunks past the head's `nch` read its first
 template <int DH, int ROWS, int WAVES> constexpr int tile_reqs() { return ROWS * DH * 2 / 1024 / WAVES; }
 template <int DH, int ROWS = BKV, int WAVES = 4>
-__device__ __forceinline__ void dma_req(int i, unsigned lds_byte, const char *src, unsigned ldb, int row0, int nrows, int nch, int wave,
-                                        int lane) {
+__device__ __forceinline__ void dma_req(int i, unsigned lds_byte, const TileRows &rows, unsigned ldb, int nch, int wave, int lane) {
   constexpr int NREQ = tile_reqs<DH, ROWS, WAVES>(), RPR = 1024 / (DH * 2), CPR = DH / 8;
   const int q = wave * NREQ + i, r = RPR * q + lane / CPR;
-  const int rg = min(row0 + r, nrows - 1);
   const int chunk = (int)((unsigned)(lane % CPR) ^ swz_both<DH>((unsigned)r));
-  dma16(lds_byte + (unsigned)q * 1024u, (unsigned)rg * ldb + (unsigned)(chunk < nch ? chunk : 0) * 16u, src);
+  dma16(lds_byte + (unsigned)q * 1024u, (unsigned)min(r, rows.more) * ldb + (unsigned)(chunk < nch ? chunk : 0) * 16u, rows.at);
 }
 template <int DH, int ROWS = BKV, int WAVES = 4>
 __device__ __forceinline__ void dma_tile(unsigned lds_byte, const char *src, unsigned ldb, int row0, int nrows, int nch, int wave, int lane) {
+  const TileRows rows = tile_rows(src, ldb, row0, nrows);
 #pragma unroll
-  for (int i = 0; i < tile_reqs<DH, ROWS, WAVES>(); ++i) dma_req<DH, ROWS, WAVES>(i, lds_byte, src, ldb, row0, nrows, nch, wave, lane);
+  for (int i = 0; i < tile_reqs<DH, ROWS, WAVES>(); ++i) dma_req<DH, ROWS, WAVES>(i, lds_byte, rows, ldb, nch, wave, lane);
 }
 // elements 16 kd + 8 (lane / 32) .. of a row as an operand fragment, zeros past the head
 __device__ __forceinline__ bf16x8 row_frag(const bf16 *row, int kd, int hh, int dh) {

@@ -276,14 +276,14 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void window_fwd_kernel(Windo
 #pragma unroll
       for (int u = 0; u < n; ++u) mx = fmaxf(mx, sv[e0 + u]);
     };
-    const int jn = kt.first_key(t + 1), jnn = kt.first_key(t + 2);
+    const int jn = kt.first_key(t + 1);
+    const TileRows kn = tile_rows(kb, ldkb, kt.first_key(t + 2), len), vn = tile_rows(vb, ldvb, jn, len);   // (past the walk's end: rows it has, which nobody reads)
     if (MORE) { zero(nxt[0]); zero(nxt[1]); ld_k(KN, 0, 0, 0); ld_k(KN, 1, 1, 0); }
 #pragma unroll
     for (int kd = 0; kd < NK; ++kd) {
       if (MORE) {
-        // (past the walk's end the requests read rows it has, and nobody reads them)
-        if (kd < NK / 2) dma_req<DH>(kd, PAR * TILE, kb, ldkb, jnn, len, nch, wave, lane);
-        else dma_req<DH>(kd - NK / 2, VOFF + (PAR ^ 1) * TILE, vb, ldvb, jn, len, nch, wave, lane);
+        if (kd < NK / 2) dma_req<DH>(kd, PAR * TILE, kn, ldkb, nch, wave, lane);
+        else dma_req<DH>(kd - NK / 2, VOFF + (PAR ^ 1) * TILE, vn, ldvb, nch, wave, lane);
         const bf16x8 ka = fx[0], kb2 = fx[1];
         if (kd + 1 < NK) { ld_k(KN, 0, 0, kd + 1); ld_k(KN, 1, 1, kd + 1); }
         nxt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[kd], nxt[0], 0, 0, 0);
@@ -526,15 +526,15 @@ template <int DH> hipError_t bwd_launch(const WindowArgs &a, hipStream_t s) {
   return e != hipSuccess ? e : launch_window_dkv(a, a.ws, (float *)((char *)a.ws + dots_bytes(a)), s);
 }
 
-bool fits(const void *p, long ld, int S) {
-  return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && (uint64_t)S * (uint64_t)ld * 2 < 0xffffffffull - 4096;
+bool fits(const void *p, long ld) {
+  return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1 << 25);   // (a tile's 64 rows in 32-bit offsets)
 }
 
 }  // namespace
 
 bool window_mfma_supported(const WindowArgs &a) {
-  return a.dh <= 128 && fits(a.q, a.ldq, a.S) && fits(a.k, a.ldk, a.S) && fits(a.v, a.ldv, a.S) && fits(a.o, a.ldo, a.S) &&
-         fits(a.o_in, a.ldo, a.S) && fits(a.d_o, a.ldo, a.S) && fits(a.dq, a.ldq, a.S) && fits(a.dk, a.ldk, a.S) && fits(a.dv, a.ldv, a.S) &&
+  return a.dh <= 128 && fits(a.q, a.ldq) && fits(a.k, a.ldk) && fits(a.v, a.ldv) && fits(a.o, a.ldo) &&
+         fits(a.o_in, a.ldo) && fits(a.d_o, a.ldo) && fits(a.dq, a.ldq) && fits(a.dk, a.ldk) && fits(a.dv, a.ldv) &&
          ((uintptr_t)a.ws & 15) == 0;
 }
 size_t window_mfma_ws_bytes(const WindowArgs &a) {
