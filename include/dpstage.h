@@ -650,10 +650,10 @@ dp_status dp_op_cross_attention_bwd(int32_t dtype, int32_t B, int32_t Sq, int32_
  * (dtype, [head_dim], overwritten; not touched where the gain is NULL).  ws: device workspace of
  * dp_op_qk_rotary_workspace_bytes bytes, for gains' gradients only.
  * q_out may be q and dq may be dq_out (the same rows), k likewise; no other overlap.  head_dim is
- * even and at most 1024 (DP_E_UNSUPPORTED otherwise).  Any alignment: vector accesses where
- * head_dim, rot_dim and the strides are multiples of 8 and pointers 16-byte aligned, element by
- * element otherwise.  No rows: nothing is read, gains' gradients become zero.  Heads of one kind
- * only: the other count 0, its pointers NULL. */
+ * even and at most 1024, rows and heads below 2^30 (DP_E_UNSUPPORTED otherwise).  Any alignment:
+ * vector accesses where head_dim, rot_dim and the strides are multiples of 8 and pointers 16-byte
+ * aligned, element by element otherwise.  No rows: nothing is read, gains' gradients become zero.
+ * Heads of one kind only: the other count 0, its pointers NULL. */
 typedef struct {
   int32_t rows, seq, q_heads, kv_heads, head_dim, rot_dim, interleaved;
   float eps, scale;
@@ -684,10 +684,11 @@ dp_status dp_op_qk_rotary_bwd(int32_t dtype, const dp_qk_rotary *shape, const vo
  * overlap of an output with anything.  Sums and statistics fp32, results rounded once (in bf16 the
  * probabilities and the logits' gradients are rounded to bf16 for the products they go into); the
  * same bits at every call.  A key or value that is not finite may spread to any row of its sample
- * (hidden keys meet it with a weight of zero), not to other samples.  head_dim is a multiple of 8 and at most 256 (DP_E_UNSUPPORTED
- * otherwise).  Any alignment; the matrix cores take head dimensions up to 128 with pointers 16-byte
- * aligned, strides that are multiples of 16 bytes and samples that span less than 4 GiB, everything
- * else goes to vector-ALU kernels 20 to 100 times slower. */
+ * (hidden keys meet it with a weight of zero), not to other samples.  head_dim is a multiple of 8
+ * and at most 256, batch * seq below 2^30, batch * q_heads * seq below 2^29 and batch * q_heads
+ * below 2^23 (DP_E_UNSUPPORTED otherwise).  Any alignment; the matrix cores take head dimensions up
+ * to 128 with pointers 16-byte aligned and strides that are multiples of 16 bytes (in bf16 below
+ * 64 MiB), everything else goes to vector-ALU kernels many times slower. */
 typedef struct {
   int32_t batch, seq, q_heads, kv_heads, head_dim, window, sinks;
   float scale;

@@ -298,6 +298,7 @@ static dp_status rotary_args(const char *what, int32_t dtype, const dp_qk_rotary
   if (c->ldq_in < wq || c->ldq_out < wq || c->ldk_in < wk || c->ldk_out < wk)
     return fail(DP_E_INVAL, "%s: a row stride is shorter than the row's heads", what);
   if (c->rows > 0 && c->rot_dim > 0 && c->q_heads + c->kv_heads > 0 && !inv_freq) return fail(DP_E_INVAL, "%s: inv_freq is null", what);
+  if (c->rows > INT32_MAX / 2 || (int64_t)c->q_heads + c->kv_heads > INT32_MAX / 2) return fail(DP_E_UNSUPPORTED, "%s: 2^30 rows or heads, or more", what);
   *p = dp::RotaryArgs{};
   p->rows = c->rows; p->seq = c->seq; p->nq = c->q_heads; p->nk = c->kv_heads; p->dh = c->head_dim;
   p->half = c->rot_dim / 2; p->interleaved = c->interleaved; p->eps = c->eps; p->scale = c->scale;
@@ -347,8 +348,10 @@ static dp_status window_args(const char *what, int32_t dtype, const dp_window_at
   if (c->head_dim % 8 || c->head_dim > 256) return fail(DP_E_UNSUPPORTED, "%s: head_dim must be a multiple of 8, <= 256", what);
   const int64_t wq = (int64_t)c->q_heads * c->head_dim, wk = (int64_t)c->kv_heads * c->head_dim;
   if (c->ldq < wq || c->ldo < wq || c->ldk < wk || c->ldv < wk) return fail(DP_E_INVAL, "%s: a row stride is shorter than the row's heads", what);
-  if ((int64_t)c->batch * c->seq > INT32_MAX || (int64_t)c->batch * c->q_heads > INT32_MAX / 64)
-    return fail(DP_E_UNSUPPORTED, "%s: more than 2^31 rows", what);
+  if ((int64_t)c->batch * c->seq > INT32_MAX / 2) return fail(DP_E_UNSUPPORTED, "%s: 2^30 rows or more", what);
+  // (a launch counts its threads in 32 bits: 512 for 64 rows of a head at most)
+  if ((int64_t)c->batch * c->q_heads >= 1 << 23 || (int64_t)c->batch * c->q_heads * (((int64_t)c->seq + 63) / 64) >= 1 << 23)
+    return fail(DP_E_UNSUPPORTED, "%s: 2^29 rows of query heads or more, or 2^23 heads", what);
   *a = dp::WindowArgs{};
   a->B = c->batch; a->S = c->seq; a->nq = c->q_heads; a->nk = c->kv_heads; a->dh = c->head_dim;
   a->window = c->window; a->sinks = c->sinks; a->scale = c->scale;

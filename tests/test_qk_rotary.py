@@ -229,6 +229,12 @@ def bwd(s, dtype=0, **kw):
     return B.lib().dp_op_qk_rotary_bwd(dtype, C.byref(s), *(a[n] for n in ("dqo", "dko", "q", "k", "qg", "kg", "freq", "pos", "dq", "dk", "dqg", "dkg", "ws")), None)
 
 
+def test_sizes_past_32_bits():
+    far = dict(ldq_in=1 << 40, ldk_in=1 << 40, ldq_out=1 << 40, ldk_out=1 << 40)
+    for kw in (dict(rows=2 ** 31 - 1), dict(rows=2 ** 30), dict(q_heads=2 ** 30, kv_heads=2 ** 30), dict(q_heads=0, kv_heads=2 ** 31 - 1)):
+        assert fwd(shape(**kw, **far)) == -7 and bwd(shape(**kw, **far)) == -7, kw
+
+
 def test_refusals():
     inval, unsupported = -1, -7
     assert fwd(None) == inval and fwd(shape(), dtype=2) == inval

@@ -393,6 +393,16 @@ def test_refusals():
     assert bwd(shape(batch=0), **nothing, d_o=None, dq=None, dk=None, dv=None, ws=None) == 0
 
 
+def test_sizes_past_the_launches():
+    """What 32-bit rows, or the threads of one launch, do not count is refused before anything is read."""
+    wide = dict(ldq=1 << 40, ldk=1 << 40, ldv=1 << 40, ldo=1 << 40)
+    for kw in (dict(batch=1, seq=2 ** 31 - 1), dict(batch=1, seq=2 ** 30 + 1), dict(batch=2 ** 20, seq=2 ** 11), dict(batch=2 ** 22, seq=1),
+               dict(batch=1, seq=2 ** 29, q_heads=2, kv_heads=1), dict(batch=1, seq=1, q_heads=2 ** 30, kv_heads=1), dict(batch=2 ** 31 - 1, seq=1)):
+        assert fwd(shape(**kw, **wide)) == -7 and bwd(shape(**kw, **wide)) == -7, kw
+        assert B.lib().dp_op_window_attention_workspace_bytes(1, C.byref(shape(**kw, **wide))) == 0
+    assert B.lib().dp_op_window_attention_workspace_bytes(1, C.byref(shape(batch=1, seq=2 ** 26, **wide))) > 0
+
+
 def test_binding_refuses_tensors_of_the_host():
     t = torch.zeros(4, 2, 64)
     with pytest.raises(B.DpError) as e:
