@@ -272,7 +272,7 @@ __global__ __launch_bounds__(THREADS, ND <= 2 ? 3 : 2) void window_dkv_f32_kerne
       __syncthreads();
       if (half + 1 < n1) ask(half + 1);
       const uint32_t hidden = hidden_queries(kj, ib, a.window, a.sinks);
-#pragma unroll
+#pragma unroll (ND == 4 ? 1 : 2)   // (128 columns: both at once spill)
       for (int u = 0; u < 2; ++u) {
         const uint32_t h16 = hidden >> (16 * u);
         if (ib + 16 * u >= len || !any_seen(h16)) continue;
