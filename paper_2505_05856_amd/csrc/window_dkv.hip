@@ -5,9 +5,12 @@ namespace dp {
 
 namespace {
 
-// Block: 128 keys of a key head and 8 waves: wave w holds keys 32 (w % 4) .. and takes one half (32 queries) of every tile, so two
-// waves of a SIMD work on the same keys and each has the instructions of one block of 32 x 32 to issue beside the other's.
-// dK, dV stand in the accumulators of both and are added at the end.
+// Block: 128 keys of a key head and 8 waves: each holds 32 keys and takes one half (32 queries) of every tile, so the two waves of a
+// SIMD have blocks of 32 x 32 of their own to issue beside each other's, and leave out those that the mask hides whole.  dK and dV
+// of the two halves are added at the end.  256 registers a wave at 128 columns: 128 of sums, 32 of K; V's fragments stand in LDS.
+// 8 x 2048 tokens of 32 + 8 heads of 128, window 512: 385 us where four waves with K and V in registers took 427 (16384 tokens of
+// 4 + 1 heads, window 4096: 343 both; 284 with the walks dealt as they are now).  Per tile of 64 queries and 128 keys the products
+// take 2048 clocks of a SIMD and the LDS reads 1700, of about 4400: a barrier a tile, and blocks of a tile that are not alike.
 template <int DH>
 __global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
                                                             float *__restrict__ sums) {

@@ -1,10 +1,11 @@
 // Sliding-window attention on the matrix cores (bf16 in, fp32 accumulate): query i of a sample sees key j when j <= i < len and
-// (i - j < window or j < sinks).  The tiles, layouts and pipelines are those of the full attention; what is different:
+// (i - j < window or j < sinks).  The tiles and layouts are those of the full attention; what is different:
 //
-// - A block of 128 queries walks two runs of 64-key tiles, those that hold the first keys and those of its window, as one list:
-//   the loads of the second run's start are in flight while the first run ends.
-// - Which keys of a tile a lane's query sees is a 32-bit word (three shifts), from which each logit takes a bit: two
-//   instructions a logit, as a causal mask alone would take, and only in tiles that hold hidden keys.
+// - A block of 128 queries walks two runs of key tiles, those that hold the first keys and those of its window, as one list: the
+//   loads of the second run's start are in flight while the first run ends.
+// - Which keys of 32 a lane's query sees is a 32-bit word (three shifts), from which each logit takes a bit: two instructions a
+//   logit, as a causal mask alone would take, and only where 32 keys hold one that is hidden from one of a wave's queries.  32
+//   keys that are hidden from all of them are passed over (dQ, dK and dV, and the forward of short windows).
 // - Query heads that share a key head are separate blocks forward and for dQ (next to each other, so one L2 serves their keys);
 //   dK and dV walk the queries of all of them, tile after tile, so no gradient is added up outside a block ...
 // - ... unless that leaves CUs idle, or keys are seen by every later query (the first ones): such a walk is cut into parts of
@@ -12,6 +13,15 @@
 // - Rows past a sample's length are never read (tiles end with copies of the last row, whose products are masked) and become 0.
 // - Head dimensions of 8..128: kernels for 64 and 128 columns; columns past the head are zeros on the side that waits in
 //   registers and copies of the first ones in LDS, and are not stored.
+//
+// Measured at 8 x 2048 tokens of 32 + 8 heads of 128, window 512, 16 first keys: 175 us forward (124 GFLOP for the pairs that are
+// seen, 705 TFLOP/s, where a large matrix product reaches 1606) and 610 backward (505 TFLOP/s of the formula's; S and dP are taken
+// twice); 16384 tokens of 4 + 1 heads, window 4096: 129 (930 TFLOP/s) and 450.  Of a SIMD's time forward, dQ, dK/dV there the
+// matrix pipe works 35, 34 and 30 % (46, 48 and 38 % at the long window), the vector ALU 44, 33 and 20 %, LDS 20, 19 and 24 %:
+// none of them bounds the kernels alone.  The rest are a wave's own dependences, products to softmax to products, which two or
+// three waves a SIMD do not fill, blocks' starts and ends, and tiles of which the mask leaves a part.
+// What lost: 64 rows a wave (half the LDS reads, one wave a SIMD: forward 224 us for 197, dQ 338 for 294, dK/dV 587 for 450);
+// loads two tiles ahead (forward 175, dK/dV 6 % slower, spills); lane offsets of the loads worked out once (no change).
 #include "window_bf16.h"
 
 #include <type_traits>
@@ -352,7 +362,9 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void window_fwd_kernel(Windo
   store_rows<DH>(smem_b + wave * (64 * DH), acc, 1.0f / l, ob + (long)iw0 * a.ldo, a.ldo, S - iw0, len - iw0, nch, lane);
 }
 
-// ------------------------------------------------------------------ backward: dQ, and the row dots <dO_i, O_i>
+// ------------------------------------------------------------------ backward: dQ, and the row dots D_i
+// 32 keys at a time, operands three steps ahead; the two waves of a SIMD hide each other's softmax.  (Two blocks of 32 in flight
+// within a wave, operands one step ahead: 8 x 2048 tokens of 32 + 8 heads of 128, window 512, 290 us for 256.)
 constexpr int kShort = 4;   // tiles
 template <int DH, bool ORDERED>
 __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrder ro) {

@@ -2,7 +2,8 @@
 // head dimensions up to 256, for the operands the matrix-core kernels do not take.  A row's keys are two runs, the first `sinks`
 // keys and the window, and only those are read, 64 at a time: a lane takes one key's logit (a dot product along its row), then
 // the wave adds the 64 weighted rows with its lanes along the head's columns.  The softmax is taken in one pass, with a running
-// maximum and sum.
+// maximum and sum.  (fp32, 64 samples of 16 tokens, 32 + 8 heads of 64: 127 us forward, 418 backward, where the matrix cores take 19
+// and 50; 40 tokens: 300 and 956 for 31 and 102; alone with one token a sample it is level.)
 #include "common.h"
 #include "kernels.h"
 
