@@ -244,7 +244,7 @@ template <int DH> hipError_t go(const WindowArgs &a, const float *drow, float *s
   hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3((unsigned)(heads * pieces_of(w))), dim3(512), smem, s, a, w, drow, sums);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || cut == 0) return e;
-  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, BROWS, DH>), dim3(heads * cut * 2 * (BROWS / 32)), dim3(256), 0, s, a, w, sums, cut);
+  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, BROWS, DH>), dim3(heads * cut * 2 * (BROWS / kSumRows)), dim3(kSumRows * DH / 4), 0, s, a, w, sums, cut);
   return hipGetLastError();
 }
 

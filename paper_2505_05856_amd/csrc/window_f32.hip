@@ -325,7 +325,7 @@ template <int ND> hipError_t bwd(const WindowArgs &a, hipStream_t s) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int cut = key_blocks_cut(w);
   if (cut == 0) return hipSuccess;
-  hipLaunchKernelGGL((window_dkv_sum_kernel<float, ROWS, 32 * ND>), dim3(heads * cut * 2 * (ROWS / 32)), dim3(256), 0, s, a, w, sums, cut);
+  hipLaunchKernelGGL((window_dkv_sum_kernel<float, ROWS, 32 * ND>), dim3(heads * cut * 2 * (ROWS / kSumRows)), dim3(kSumRows * 8 * ND), 0, s, a, w, sums, cut);
   return hipGetLastError();
 }
 int blocks_of_32(const WindowArgs &a) { return (a.dh + 31) / 32; }

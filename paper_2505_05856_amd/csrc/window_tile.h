@@ -103,12 +103,13 @@ __host__ __device__ __forceinline__ long slot_of(const KeyWork &w, long head, in
          (piece < w.parts ? (long)kb * w.parts + piece : windows + (long)kb * w.far + piece - w.parts);
 }
 
-// dK, dV of the key blocks whose walk was cut: the pieces' sums, in order.  Block: 32 keys of one of the two.
+// dK, dV of the key blocks whose walk was cut: the pieces' sums, in order.  Block: kSumRows keys of one of the two, DH / 4 lanes a key.
+constexpr int kSumRows = 8;
 template <typename T, int ROWS, int DH>
-__global__ __launch_bounds__(256) void window_dkv_sum_kernel(WindowArgs a, KeyWork w, const float *__restrict__ sums, int blocks_per_head) {
-  constexpr int LANES = DH / 4, PARTS = ROWS / 32;   // lanes a row, blocks a key block and result
+__global__ __launch_bounds__(kSumRows * DH / 4) void window_dkv_sum_kernel(WindowArgs a, KeyWork w, const float *__restrict__ sums, int blocks_per_head) {
+  constexpr int LANES = DH / 4, PARTS = ROWS / kSumRows;   // lanes a row, blocks a key block and result
   const int group = a.nq / a.nk;
-  const int row0 = (blockIdx.x % PARTS) * 32, which = (blockIdx.x / PARTS) & 1, id = blockIdx.x / (2 * PARTS);
+  const int r = (int)(blockIdx.x % PARTS) * kSumRows + (int)threadIdx.x / LANES, which = (blockIdx.x / PARTS) & 1, id = blockIdx.x / (2 * PARTS);
   const int head = id / blocks_per_head, kb = id - head * blocks_per_head;
   const int kh = head % a.nk, b = head / a.nk, len = sample_len(a, b);
   // how many of the two kinds of pieces hold anything (those from some piece on are empty)
@@ -126,22 +127,20 @@ __global__ __launch_bounds__(256) void window_dkv_sum_kernel(WindowArgs a, KeyWo
   const int col = (threadIdx.x % LANES) * 4;
   if (col >= a.dh) return;
   typedef T T4 __attribute__((ext_vector_type(4)));
-  for (int r = row0 + threadIdx.x / LANES; r < row0 + 32; r += 256 / LANES) {
-    const int j = kb * ROWS + r;
-    if (j >= a.S) return;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (j < len) {
-#pragma unroll 4
-      for (int p = 0; p < near; ++p) s += *reinterpret_cast<const f32x4 *>(pn + p * slot + r * DH + col);
-#pragma unroll 4
-      for (int p = 0; p < far; ++p) s += *reinterpret_cast<const f32x4 *>(pf + p * slot + r * DH + col);
-    }
-    T4 v;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = (T)(which == 0 ? s[u] * a.scale : s[u]);
-    T *out = which == 0 ? (T *)a.dk + ((long)b * a.S + j) * a.ldk : (T *)a.dv + ((long)b * a.S + j) * a.ldv;
-    *reinterpret_cast<T4 *>(out + (long)kh * a.dh + col) = v;
+  const int j = kb * ROWS + r;
+  if (j >= a.S) return;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (j < len) {
+#pragma unroll 8
+    for (int p = 0; p < near; ++p) s += *reinterpret_cast<const f32x4 *>(pn + p * slot + r * DH + col);
+#pragma unroll 8
+    for (int p = 0; p < far; ++p) s += *reinterpret_cast<const f32x4 *>(pf + p * slot + r * DH + col);
   }
+  T4 v;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) v[u] = (T)(which == 0 ? s[u] * a.scale : s[u]);
+  T *out = which == 0 ? (T *)a.dk + ((long)b * a.S + j) * a.ldk : (T *)a.dv + ((long)b * a.S + j) * a.ldv;
+  *reinterpret_cast<T4 *>(out + (long)kh * a.dh + col) = v;
 }
 
 size_t slots_of(const WindowArgs &a, const KeyWork &w) {
