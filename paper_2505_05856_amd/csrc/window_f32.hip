@@ -308,7 +308,7 @@ __global__ __launch_bounds__(THREADS, ND <= 2 ? 3 : 2) void window_dkv_f32_kerne
 }
 
 // (Workgroups at once: two a CU at up to 64 columns, else one.  An item is about 8 us at 64 columns, a slot two [64][64] arrays.)
-KeyWork work_of(const WindowArgs &a) { return key_work<ROWS>(a, kCus * (a.dh <= 64 ? 2 : 1), Costs{0.4, 0.002, 0.4}); }
+KeyWork work_of(const WindowArgs &a) { return key_work<ROWS>(a, kCus * (a.dh <= 64 ? 2 : 1), Costs{0.4, 0.002, 0.4}, (int)sizeof(float)); }
 
 template <int ND> hipError_t fwd(const WindowArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((window_fwd_f32_kernel<ND>), dim3((a.S + ROWS - 1) / ROWS * a.nq * a.B), dim3(THREADS), 0, s, a);

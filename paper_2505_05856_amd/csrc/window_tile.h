@@ -52,8 +52,9 @@ __device__ __forceinline__ int sample_len(const WindowArgs &a, int b) {
 // How the walks over query tiles (64 queries) are cut.  Key block kb (ROWS keys) of a key head walks, for each query head of its
 // group, the tiles from its own first to the end of its window: `parts` pieces.  Key blocks below `first` hold keys that all
 // later queries see: the rest of the sequence, `far` pieces more.
-// Key blocks below `full` have a whole window of queries after them, the others a shorter walk.
-struct KeyWork { int key_blocks, parts, first, far, full; };
+// Key blocks below `full` have a whole window of queries after them, the others a shorter walk.  `together`: how many heads' shorter
+// walks an XCD takes at a time.
+struct KeyWork { int key_blocks, parts, first, far, full, together; };
 
 struct Walk { int t0, nt, begin, end; };   // query tiles t0 .. t0+nt-1 of each head in turn; items begin .. end-1 of that list
 template <int ROWS> __host__ __device__ __forceinline__ Walk walk_of(const KeyWork &w, int kb, int piece, int len, int window, int group) {
@@ -72,9 +73,10 @@ template <int ROWS> __host__ __device__ __forceinline__ Walk walk_of(const KeyWo
 }
 // Which piece a workgroup takes.  Workgroup i runs on XCD i % 8, and an XCD starts its own in order.  Whole walks come first, a head
 // (its far pieces, then its key blocks) after the other: an XCD gets all of a head's, or where the heads do not go round evenly
-// four in a row, so that those that share queries share an L2.  The shorter walks follow, one by one in falling length: they fill
-// the holes that the last whole ones leave, on every XCD alike.  (Contiguous shares in head order gave one XCD the ends of the
-// sequence alone: 16384 tokens of 4 + 1 heads, window 4096, took 1.2 times as long.)
+// four in a row, so that those that share queries share an L2.  The shorter walks follow, in falling length: they fill the holes
+// that the last whole ones leave, on every XCD alike.  (Contiguous shares in head order gave one XCD the ends of the sequence
+// alone: 16384 tokens of 4 + 1 heads, window 4096, took 1.2 times as long.)  They go one by one to the XCDs, or, heads going round
+// evenly, those of an XCD's own heads, as many heads at a time as fill its CUs or, if that is more, its L2 with their queries.
 struct Piece { int head, kb, piece; };
 __device__ __forceinline__ Piece piece_at(const KeyWork &w, int i, int heads) {
   const int nfar = w.first * w.far, per_head = nfar + w.full * w.parts, whole = heads * per_head;
@@ -87,8 +89,17 @@ __device__ __forceinline__ Piece piece_at(const KeyWork &w, int i, int heads) {
     p.kb = id < nfar ? id / w.far : (id - nfar) / w.parts;
     p.piece = id < nfar ? w.parts + id % w.far : (id - nfar) % w.parts;
   } else {
-    const int id = i - whole, row = id / heads;
-    p.head = id - row * heads;
+    const int id = i - whole, rows = (w.key_blocks - w.full) * w.parts;
+    int first = 0, step = 1, n = heads, at = id;   // heads first, first + step ..: n of them together
+    if (heads % 8 == 0) {
+      const int own = heads / 8, set = id / 8 / (w.together * rows);
+      first = id % 8 + 8 * w.together * set;
+      step = 8;
+      n = min(w.together, own - w.together * set);
+      at = id / 8 - w.together * set * rows;
+    }
+    const int row = at / n;
+    p.head = first + step * (at - row * n);
     p.kb = w.full + row / w.parts;
     p.piece = row % w.parts;
   }
@@ -157,7 +168,7 @@ long pieces_of(const KeyWork &w) { return (long)w.key_blocks * w.parts + (long)w
 // A slot is written and read once more, and adding up is a launch: `slot` and `launch`.  More than kSlots slots of workspace are
 // taken only where no cut does with fewer.
 struct Costs { double start, slot, launch; };   // in items
-template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once, const Costs &cost) {
+template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once, const Costs &cost, int bytes) {
   constexpr size_t kSlots = 4096;
   constexpr int R = ROWS / BKV;
   const int group = a.nq / a.nk, tiles = (a.S + BKV - 1) / BKV, in_window = (ROWS + a.window - 2) / BKV + 1;   // (as walk_of has them)
@@ -196,6 +207,15 @@ template <int ROWS> KeyWork key_work(const WindowArgs &a, int at_once, const Cos
   if (w.first > 0)   // longer pieces for the rest of the sequence than the windows have
     for (int n = 2; (long)walk * (n / 2) < rest; n *= 2) consider((long)walk * n < rest ? walk * n : rest);
   for (int parts = 2; parts <= 64 && parts <= walk; ++parts) consider((walk + parts - 1) / parts);
+  // heads whose shorter walks go together on an XCD: sets of one size that fill its CUs, or its L2 (two tensors) if that is more
+  const int own = a.B * a.nk / 8, rows = (best.key_blocks - best.full) * best.parts;
+  if (own > 0 && rows > 0) {
+    const long streamed = (long)a.S * group * a.dh * 2 * bytes;
+    long want = (at_once / 8 + rows - 1) / rows;
+    if ((4l << 20) / streamed > want) want = (4l << 20) / streamed;
+    const long sets = want >= own ? 1 : (own + want - 1) / want;
+    best.together = (int)((own + sets - 1) / sets);
+  }
   return best;
 }
 
