@@ -68,8 +68,11 @@ __device__ __forceinline__ void zero_rows(bf16 *dst, long ld, int r0, int r1, in
 }
 
 inline int columns(const WindowArgs &a) { return a.dh <= 64 ? 64 : 128; }
-// (A workgroup a CU.  An item is about 2 us; a slot is two [128][128] arrays, a 40th of an item of the whole chip's time.)
-inline KeyWork work_of(const WindowArgs &a) { return key_work<BROWS>(a, kCus, Costs{3, 0.025, 2}, (int)sizeof(bf16)); }
+// Keys of a workgroup of dK, dV, and how its walks are cut
+template <int DH> constexpr int key_rows() { return DH == 64 ? 64 : 128; }
+template <int DH> KeyWork work_of(const WindowArgs &a) {
+  return key_work<key_rows<DH>()>(a, DH == 64 ? 2 * kCus : kCus, Costs{3, 0.025, 2}, (int)sizeof(bf16));
+}
 
 }  // namespace
 

@@ -5,19 +5,21 @@ namespace dp {
 
 namespace {
 
-// Block: 128 keys of a key head and 8 waves: each holds 32 keys and takes one half (32 queries) of every tile, so the two waves of a
-// SIMD have blocks of 32 x 32 of their own to issue beside each other's, and leave out those that the mask hides whole.  dK and dV
-// of the two halves are added at the end.  256 registers a wave at 128 columns: 128 of sums, 32 of K; V's fragments stand in LDS.
-// 8 x 2048 tokens of 32 + 8 heads of 128, window 512: 385 us where four waves with K and V in registers took 427 (16384 tokens of
-// 4 + 1 heads, window 4096: 343 both; 284 with the walks dealt as they are now).  Per tile of 64 queries and 128 keys the products
-// take 2048 clocks of a SIMD and the LDS reads 1700, of about 4400: a barrier a tile, and blocks of a tile that are not alike.
+// Block: 128 keys of a key head and 8 waves (64 columns: 64 keys, 4 waves, two blocks a CU): each wave holds 32 keys and takes one
+// half (32 queries) of every tile, so the two waves of a SIMD have blocks of 32 x 32 of their own to issue beside each other's, and
+// leave out those that the mask hides whole.  dK and dV of the two halves are added at the end.  256 registers a wave at 128
+// columns: 128 of sums, 32 of K; V's fragments stand in LDS.
+// 8 x 2048 tokens of 32 + 8 heads of 128, window 512: 345 us where four waves with K and V in registers took 427.  Per tile of 64
+// queries and 128 keys the products take 2048 clocks of a SIMD and the LDS reads 1700, of about 4000: a barrier a tile, and blocks
+// of a tile that are not alike.  64 columns by 128 keys and 8 waves: 8 x 2048 tokens of 32 + 8 heads, window 256, backward 133 us
+// for 120, 4096 tokens of 8 heads, window 512, 51 for 41 (a block's start and end had the CU to themselves).
 template <int DH>
-__global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
+__global__ __launch_bounds__(4 * key_rows<DH>(), 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
                                                             float *__restrict__ sums) {
-  constexpr int ND = DH / 32, NK = DH / 16;
+  constexpr int ND = DH / 32, NK = DH / 16, ROWS = key_rows<DH>(), GROUPS = ROWS / 32, WAVES = 2 * GROUPS;
   // LDS, in bytes: [stage 0: Q, dO][stage 1: Q, dO][V of the block's keys][stage 0: lse, row dots][stage 1: lse, row dots]
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
-  constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE, VBASE = 2 * STAGE, FBASE = VBASE + BROWS * DH * 2, FSTAGE = 8 * BKV, ROWB = DH * 2;
+  constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE, VBASE = 2 * STAGE, FBASE = VBASE + ROWS * DH * 2, FSTAGE = 8 * BKV, ROWB = DH * 2;
 
   const int S = a.S, nch = a.dh / 8, group = a.nq / a.nk;
   const Piece at = piece_at(w, blockIdx.x, a.B * a.nk);
@@ -26,18 +28,18 @@ __global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWor
   const int len = sample_len(a, b);
   const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = wave >> 2, kg = half ? 3 - (wave & 3) : wave & 3;   // (the halves of a SIMD's pair differ in keys: edges are as uneven)
-  const int j0 = kb * BROWS, jw0 = j0 + kg * 32, kj = jw0 + (lane & 31);
+  const int half = wave / GROUPS, kg = half ? WAVES - 1 - wave : wave;   // (the halves of a SIMD's pair differ in keys: edges are as uneven)
+  const int j0 = kb * ROWS, jw0 = j0 + kg * 32, kj = jw0 + (lane & 31);
   const long slot = slot_of(w, head, kb, piece);
   bf16 *dkb = (bf16 *)a.dk + (long)b * S * a.ldk + (long)kh * a.dh, *dvb = (bf16 *)a.dv + (long)b * S * a.ldv + (long)kh * a.dh;
   if (j0 >= len) {
     if (slot < 0) {
-      zero_rows(dkb, a.ldk, j0, min(j0 + BROWS, S), nch);
-      zero_rows(dvb, a.ldv, j0, min(j0 + BROWS, S), nch);
+      zero_rows(dkb, a.ldk, j0, min(j0 + ROWS, S), nch);
+      zero_rows(dvb, a.ldv, j0, min(j0 + ROWS, S), nch);
     }
     return;
   }
-  const Walk walk = walk_of<BROWS>(w, kb, piece, len, a.window, group);
+  const Walk walk = walk_of<ROWS>(w, kb, piece, len, a.window, group);
   if (walk.begin == walk.end) return;   // (a piece of several: the kernel that adds them up knows)
   const bf16 *krow = (const bf16 *)a.k + ((long)b * S + min(kj, len - 1)) * a.ldk + (long)kh * a.dh;
   const bf16 *vrow = (const bf16 *)a.v + ((long)b * S + min(kj, len - 1)) * a.ldv + (long)kh * a.dh;
@@ -58,8 +60,8 @@ __global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWor
   int i_next = 0;   // first query of the tile fetched last
   auto fetch = [&](unsigned buf) {
     i_next = (walk.t0 + t) * BKV;
-    dma_tile<DH, BKV, 8>(buf, qsrc, ldqb, i_next, len, nch, wave, lane);
-    dma_tile<DH, BKV, 8>(buf + TILE, osrc, ldob, i_next, len, nch, wave, lane);
+    dma_tile<DH, BKV, WAVES>(buf, qsrc, ldqb, i_next, len, nch, wave, lane);
+    dma_tile<DH, BKV, WAVES>(buf + TILE, osrc, ldob, i_next, len, nch, wave, lane);
     if (wave < 2) sl = fsrc[min(i_next + lane, len - 1)];
     if (++t == walk.nt) { t = 0; qsrc += 2 * a.dh; osrc += 2 * a.dh; fsrc += S; }
   };
@@ -182,8 +184,8 @@ __global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWor
 
   // a wave's dK, dV and those of the other half for the same keys are added through LDS, half of the columns at a time: the first
   // half of the waves ends with dK, the second with dV
-  float *mine = reinterpret_cast<float *>(smem_b) + (half * 4 + kg) * (ND / 2 * 1024) + lane * 4;
-  const float *other = reinterpret_cast<const float *>(smem_b) + ((half ^ 1) * 4 + kg) * (ND / 2 * 1024) + lane * 4;
+  float *mine = reinterpret_cast<float *>(smem_b) + (half * GROUPS + kg) * (ND / 2 * 1024) + lane * 4;
+  const float *other = reinterpret_cast<const float *>(smem_b) + ((half ^ 1) * GROUPS + kg) * (ND / 2 * 1024) + lane * 4;
   auto give = [&](const f32x16 &v, int d) {
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4) {
@@ -220,7 +222,7 @@ __global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWor
       return;
     }
     // sums of this piece: a lane's key is a row, its four consecutive columns one store
-    float *to = sums + slot * (2 * BROWS * DH) + half * (BROWS * DH) + (kg * 32 + (lane & 31)) * DH + 4 * hh;
+    float *to = sums + slot * (2 * ROWS * DH) + half * (ROWS * DH) + (kg * 32 + (lane & 31)) * DH + 4 * hh;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -234,17 +236,17 @@ __global__ __launch_bounds__(512, 2) void window_dkv_kernel(WindowArgs a, KeyWor
 }
 
 template <int DH> hipError_t go(const WindowArgs &a, const float *drow, float *sums, hipStream_t s) {
-  constexpr size_t smem = (4 * (size_t)BKV + BROWS) * DH * sizeof(bf16) + 4 * BKV * sizeof(float);
+  constexpr size_t smem = (4 * (size_t)BKV + key_rows<DH>()) * DH * sizeof(bf16) + 4 * BKV * sizeof(float);
   if (smem > 64 * 1024) {   // (beyond that it has to be asked for, on every device)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(window_dkv_kernel<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != hipSuccess) return e;
   }
-  const KeyWork w = work_of(a);
+  const KeyWork w = work_of<DH>(a);
   const int heads = a.B * a.nk, cut = key_blocks_cut(w);
-  hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3((unsigned)(heads * pieces_of(w))), dim3(512), smem, s, a, w, drow, sums);
+  hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3((unsigned)(heads * pieces_of(w))), dim3(4 * key_rows<DH>()), smem, s, a, w, drow, sums);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || cut == 0) return e;
-  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, BROWS, DH>), dim3(heads * cut * 2 * (BROWS / kSumRows)), dim3(kSumRows * DH / 4), 0, s, a, w, sums, cut);
+  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, key_rows<DH>(), DH>), dim3(heads * cut * 2 * (key_rows<DH>() / kSumRows)), dim3(kSumRows * DH / 4), 0, s, a, w, sums, cut);
   return hipGetLastError();
 }
 

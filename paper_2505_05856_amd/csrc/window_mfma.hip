@@ -550,7 +550,9 @@ bool window_mfma_supported(const WindowArgs &a) {
          ((uintptr_t)a.ws & 15) == 0;
 }
 size_t window_mfma_ws_bytes(const WindowArgs &a) {
-  return a.dh > 128 ? 0 : dots_bytes(a) + slots_of(a, work_of(a)) * 2 * BROWS * (size_t)columns(a) * sizeof(float);
+  if (a.dh > 128) return 0;
+  const size_t floats = columns(a) == 64 ? slots_of(a, work_of<64>(a)) * key_rows<64>() : slots_of(a, work_of<128>(a)) * key_rows<128>();
+  return dots_bytes(a) + floats * 2 * (size_t)columns(a) * sizeof(float);
 }
 hipError_t launch_window_fwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? fwd_launch<64>(a, s) : fwd_launch<128>(a, s); }
 hipError_t launch_window_bwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? bwd_launch<64>(a, s) : bwd_launch<128>(a, s); }
