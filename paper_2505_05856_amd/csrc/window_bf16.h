@@ -68,10 +68,17 @@ __device__ __forceinline__ void zero_rows(bf16 *dst, long ld, int r0, int r1, in
 }
 
 inline int columns(const WindowArgs &a) { return a.dh <= 64 ? 64 : 128; }
-// Keys of a workgroup of dK, dV, and how its walks are cut
-template <int DH> constexpr int key_rows() { return DH == 64 ? 64 : 128; }
-template <int DH> KeyWork work_of(const WindowArgs &a) {
-  return key_work<key_rows<DH>()>(a, DH == 64 ? 2 * kCus : kCus, Costs{3, 0.025, 2}, (int)sizeof(bf16));
+// Keys of a workgroup of dK, dV: 128, eight waves that have a CU to themselves and bring every tile once, or, where walks are short,
+// 64 and four waves, two workgroups a CU, of which one works while the other starts or ends.  Backward, us, 128 and 64 keys:
+//   heads of 128: 200 tokens, 8 + 2 heads, window 64: 34.1, 30.1    2 x 700, 8 + 2, 128: 44.0, 37.7    4096, 8 + 8, 512: 71.9, 60.8
+//                 4 x 2048, 32 + 8, 256: 221, 211    8 x 2048, 32 + 8, 512: 587, 575    4096, 8 + 2, 1024: 88, 92    16384, 4 + 1, 4096: 418, 449
+//   heads of 64:  2 x 700, 8 + 2, 128: 33.0, 27.8    4096, 8 + 8, 512: 50.7, 41.2    4 x 2048, 32 + 8, 256: 133, 121    16384, 4 + 1, 4096: 257, 268
+inline int key_rows(const WindowArgs &a) {
+  const int tiles = (a.S + BKV - 1) / BKV, in_window = (BROWS + a.window - 2) / BKV + 1;
+  return (long)(a.nq / a.nk) * (tiles < in_window ? tiles : in_window) <= 40 ? 64 : 128;   // (items: tiles of 64 queries of a head)
+}
+template <int ROWS> KeyWork work_of(const WindowArgs &a) {
+  return key_work<ROWS>(a, ROWS == 64 ? 2 * kCus : kCus, Costs{3, 0.025, 2}, (int)sizeof(bf16));
 }
 
 }  // namespace

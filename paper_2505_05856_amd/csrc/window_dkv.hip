@@ -5,21 +5,21 @@ namespace dp {
 
 namespace {
 
-// Block: 128 keys of a key head and 8 waves (64 columns: 64 keys, 4 waves, two blocks a CU): each wave holds 32 keys and takes one
-// half (32 queries) of every tile, so the two waves of a SIMD have blocks of 32 x 32 of their own to issue beside each other's, and
-// leave out those that the mask hides whole.  dK and dV of the two halves are added at the end.  256 registers a wave at 128
-// columns: 128 of sums, 32 of K; V's fragments stand in LDS.
-// 8 x 2048 tokens of 32 + 8 heads of 128, window 512: 345 us where four waves with K and V in registers took 427.  Per tile of 64
-// queries and 128 keys the products take 2048 clocks of a SIMD and the LDS reads 1700, of about 4000: a barrier a tile, and blocks
-// of a tile that are not alike.  64 columns by 128 keys and 8 waves: 8 x 2048 tokens of 32 + 8 heads, window 256, backward 133 us
-// for 120, 4096 tokens of 8 heads, window 512, 51 for 41 (a block's start and end had the CU to themselves).
-template <int DH>
-__global__ __launch_bounds__(4 * key_rows<DH>(), 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
+// Block: ROWS keys of a key head, two waves for every 32 of them, each with one half (32 queries) of every tile: the two waves of a
+// SIMD have blocks of 32 x 32 of their own to issue beside each other's, and leave out those that the mask hides whole.  dK and dV
+// of the two halves are added at the end.  256 registers a wave at 128 columns: 128 of sums, 32 of K; V's fragments stand in LDS.
+// 8 x 2048 tokens of 32 + 8 heads of 128, window 512: 340 us where four waves a block with K and V in registers took 427.  Per tile
+// of 64 queries and 128 keys the products take 2048 clocks of a SIMD and the LDS reads 1700, of about 4000: a barrier a tile, and
+// blocks of a tile that are not alike.
+// fragments of 16 columns of V that stand in LDS: all, but where two blocks of 128 columns share 160 KB
+template <int DH, int ROWS> constexpr int v_in_lds() { return DH == 128 && ROWS == 64 ? 7 : DH / 16; }
+template <int DH, int ROWS>
+__global__ __launch_bounds__(4 * ROWS, 2) void window_dkv_kernel(WindowArgs a, KeyWork w, const float *__restrict__ drow,
                                                             float *__restrict__ sums) {
-  constexpr int ND = DH / 32, NK = DH / 16, ROWS = key_rows<DH>(), GROUPS = ROWS / 32, WAVES = 2 * GROUPS;
+  constexpr int ND = DH / 32, NK = DH / 16, GROUPS = ROWS / 32, WAVES = 2 * GROUPS, VKD = v_in_lds<DH, ROWS>();
   // LDS, in bytes: [stage 0: Q, dO][stage 1: Q, dO][V of the block's keys][stage 0: lse, row dots][stage 1: lse, row dots]
   extern __shared__ __attribute__((aligned(16))) unsigned char smem_b[];
-  constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE, VBASE = 2 * STAGE, FBASE = VBASE + ROWS * DH * 2, FSTAGE = 8 * BKV, ROWB = DH * 2;
+  constexpr unsigned TILE = BKV * DH * 2, STAGE = 2 * TILE, VBASE = 2 * STAGE, FBASE = VBASE + GROUPS * VKD * 1024, FSTAGE = 8 * BKV, ROWB = DH * 2;
 
   const int S = a.S, nch = a.dh / 8, group = a.nq / a.nk;
   const Piece at = piece_at(w, blockIdx.x, a.B * a.nk);
@@ -59,6 +59,8 @@ __global__ __launch_bounds__(4 * key_rows<DH>(), 2) void window_dkv_kernel(Windo
   float sl = 0.f;
   int i_next = 0;   // first query of the tile fetched last
   auto fetch = [&](unsigned buf) {
+    int lane = tid & 63;
+    if constexpr (VKD < NK) asm volatile("" : "+v"(lane));   // (what follows from it is worked out again for every tile: no registers left)
     i_next = (walk.t0 + t) * BKV;
     dma_tile<DH, BKV, WAVES>(buf, qsrc, ldqb, i_next, len, nch, wave, lane);
     dma_tile<DH, BKV, WAVES>(buf + TILE, osrc, ldob, i_next, len, nch, wave, lane);
@@ -70,17 +72,19 @@ __global__ __launch_bounds__(4 * key_rows<DH>(), 2) void window_dkv_kernel(Windo
   };
   fetch(0u);
 
-  // fragments of the block's keys: K's in registers, V's in LDS, laid out as a tile's rows
+  // fragments of the block's keys: K's in registers, V's in LDS, one after the other
   const unsigned r = (unsigned)(lane & 31), rowb = r * ROWB + (((unsigned)hh ^ swz_both<DH>(r)) << 4);   // (element 0; 16 kd: ^ kd << 5)
-  const unsigned vrowb = VBASE + (unsigned)kg * (32 * ROWB) + rowb;
+  const unsigned vat = VBASE + (unsigned)(kg * VKD) * 1024u + (unsigned)lane * 16u;
   bf16x8 kf[NK];
 #pragma unroll
   for (int kd = 0; kd < NK; ++kd) kf[kd] = row_frag(krow, kd, hh, a.dh);
 #pragma unroll
   for (int kd = 0; kd < NK / 2; ++kd) {
     const int k2 = kd + half * (NK / 2);
-    *(lds_bf16x8 *)(uintptr_t)(vrowb ^ ((unsigned)k2 << 5)) = row_frag(vrow, k2, hh, a.dh);
+    if (k2 < VKD) *(lds_bf16x8 *)(uintptr_t)(vat + (unsigned)k2 * 1024u) = row_frag(vrow, k2, hh, a.dh);
   }
+  bf16x8 vlast;   // (what LDS has no room for)
+  if constexpr (VKD < NK) vlast = row_frag(vrow, NK - 1, hh, a.dh);
   stash(0u);
   f32x16 dk[ND], dv[ND];
 #pragma unroll
@@ -116,7 +120,7 @@ __global__ __launch_bounds__(4 * key_rows<DH>(), 2) void window_dkv_kernel(Windo
       if (i >= NK) return;
       fx[i % RING] = rows_of(row, 0u, i);
       fy[i % RING] = rows_of(row, TILE, i);
-      fv[i % RING] = rows_of(vrowb, 0u, i);
+      if (i < VKD) fv[i % RING] = *(const lds_bf16x8 *)(uintptr_t)(vat + (unsigned)i * 1024u);
     };
     auto ld_cols = [&](int i) {   // dO, Q down the rows
       if (i >= NK) return;
@@ -136,7 +140,7 @@ __global__ __launch_bounds__(4 * key_rows<DH>(), 2) void window_dkv_kernel(Windo
     for (int i = 0; i < NK; ++i) {
       ld_rows(i + AHEAD);
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[i % RING], kf[i], s, 0, 0, 0);
-      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[i % RING], fv[i % RING], dp, 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fy[i % RING], i < VKD ? fv[i % RING] : vlast, dp, 0, 0, 0);
       fence();
     }
     f32x4 l[4];
@@ -235,25 +239,27 @@ __global__ __launch_bounds__(4 * key_rows<DH>(), 2) void window_dkv_kernel(Windo
   else out(dv, 1.f, dvb, a.ldv);
 }
 
-template <int DH> hipError_t go(const WindowArgs &a, const float *drow, float *sums, hipStream_t s) {
-  constexpr size_t smem = (4 * (size_t)BKV + key_rows<DH>()) * DH * sizeof(bf16) + 4 * BKV * sizeof(float);
+template <int DH, int ROWS> hipError_t go(const WindowArgs &a, const float *drow, float *sums, hipStream_t s) {
+  constexpr size_t smem = 4 * (size_t)BKV * DH * sizeof(bf16) + ROWS / 32 * v_in_lds<DH, ROWS>() * 1024 + 4 * BKV * sizeof(float);
+  const auto kern = window_dkv_kernel<DH, ROWS>;
   if (smem > 64 * 1024) {   // (beyond that it has to be asked for, on every device)
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(window_dkv_kernel<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != hipSuccess) return e;
   }
-  const KeyWork w = work_of<DH>(a);
+  const KeyWork w = work_of<ROWS>(a);
   const int heads = a.B * a.nk, cut = key_blocks_cut(w);
-  hipLaunchKernelGGL((window_dkv_kernel<DH>), dim3((unsigned)(heads * pieces_of(w))), dim3(4 * key_rows<DH>()), smem, s, a, w, drow, sums);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(heads * pieces_of(w))), dim3(4 * ROWS), smem, s, a, w, drow, sums);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || cut == 0) return e;
-  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, key_rows<DH>(), DH>), dim3(heads * cut * 2 * (key_rows<DH>() / kSumRows)), dim3(kSumRows * DH / 4), 0, s, a, w, sums, cut);
+  hipLaunchKernelGGL((window_dkv_sum_kernel<bf16, ROWS, DH>), dim3(heads * cut * 2 * (ROWS / kSumRows)), dim3(kSumRows * DH / 4), 0, s, a, w, sums, cut);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_window_dkv(const WindowArgs &a, const float *drow, float *sums, hipStream_t s) {
-  return columns(a) == 64 ? go<64>(a, drow, sums, s) : go<128>(a, drow, sums, s);
+  if (key_rows(a) == 64) return columns(a) == 64 ? go<64, 64>(a, drow, sums, s) : go<128, 64>(a, drow, sums, s);
+  return columns(a) == 64 ? go<64, 128>(a, drow, sums, s) : go<128, 128>(a, drow, sums, s);
 }
 
 }  // namespace dp

@@ -551,8 +551,9 @@ bool window_mfma_supported(const WindowArgs &a) {
 }
 size_t window_mfma_ws_bytes(const WindowArgs &a) {
   if (a.dh > 128) return 0;
-  const size_t floats = columns(a) == 64 ? slots_of(a, work_of<64>(a)) * key_rows<64>() : slots_of(a, work_of<128>(a)) * key_rows<128>();
-  return dots_bytes(a) + floats * 2 * (size_t)columns(a) * sizeof(float);
+  const int rows = key_rows(a);
+  const size_t slots = rows == 64 ? slots_of(a, work_of<64>(a)) : slots_of(a, work_of<128>(a));
+  return dots_bytes(a) + slots * 2 * rows * (size_t)columns(a) * sizeof(float);
 }
 hipError_t launch_window_fwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? fwd_launch<64>(a, s) : fwd_launch<128>(a, s); }
 hipError_t launch_window_bwd_mfma(const WindowArgs &a, hipStream_t s) { return columns(a) == 64 ? bwd_launch<64>(a, s) : bwd_launch<128>(a, s); }

@@ -191,6 +191,14 @@ def test_walks_of_keys_dealt_and_cut(Bn, S, nq, nk, window, sinks, lens, dt):
 
 
 @gpu
+@pytest.mark.parametrize("Bn,S,nq,nk,dh,window,sinks,lens", [(1, 450, 8, 1, 128, 450, 0, None), (2, 500, 8, 1, 64, 330, 3, [500, 217]), (1, 700, 16, 2, 96, 300, 140, None),
+                                                             (3, 390, 12, 1, 40, 129, 2, [390, 64, 1]), (1, 1300, 6, 1, 128, 700, 5, None), (8, 200, 22, 2, 64, 200, 0, None)])
+def test_many_query_heads_to_a_key_head(Bn, S, nq, nk, dh, window, sinks, lens):
+    """Walks of the keys that are long because many heads share them."""
+    case(Bn, S, nq, nk, dh, window, sinks, lens=lens, packed=lens is None)
+
+
+@gpu
 @pytest.mark.parametrize("S,window", [(300, 2), (300, 5), (200, 64), (900, 200), (400, 400)])
 def test_gradients_are_rounded_twice(S, window):
     """Where a query sees few keys the rounding of O must not reach dQ and dK through <dO, O>: what is left are the rounding of dS and
