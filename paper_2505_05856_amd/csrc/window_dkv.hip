@@ -8,8 +8,8 @@ namespace {
 // Block: ROWS keys of a key head, two waves for every 32 of them, each with one half (32 queries) of every tile: the two waves of a
 // SIMD have blocks of 32 x 32 of their own to issue beside each other's, and leave out those that the mask hides whole.  dK and dV
 // of the two halves are added at the end.  256 registers a wave at 128 columns: 128 of sums, 32 of K; V's fragments stand in LDS.
-// 8 x 2048 tokens of 32 + 8 heads of 128, window 512: 340 us where four waves a block with K and V in registers took 427.  Per tile
-// of 64 queries and 128 keys the products take 2048 clocks of a SIMD and the LDS reads 1700, of about 4000: a barrier a tile, and
+// 8 x 2048 tokens of 32 + 8 heads of 128, window 512: 307 us where four waves a block with K and V in registers took 427.  Per tile
+// of 64 queries and 128 keys the products take 2048 clocks of a SIMD and the LDS reads 1700, of about 3600: a barrier a tile, and
 // blocks of a tile that are not alike.
 // fragments of 16 columns of V that stand in LDS: all, but where two blocks of 128 columns share 160 KB
 template <int DH, int ROWS> constexpr int v_in_lds() { return DH == 128 && ROWS == 64 ? 7 : DH / 16; }

@@ -15,13 +15,14 @@
 //   registers and copies of the first ones in LDS, and are not stored.
 //
 // Measured at 8 x 2048 tokens of 32 + 8 heads of 128, window 512, 16 first keys: 175 us forward (124 GFLOP for the pairs that are
-// seen, 705 TFLOP/s, where a large matrix product reaches 1606) and 610 backward (505 TFLOP/s of the formula's; S and dP are taken
-// twice); 16384 tokens of 4 + 1 heads, window 4096: 129 (930 TFLOP/s) and 450.  Of a SIMD's time forward, dQ, dK/dV there the
-// matrix pipe works 35, 34 and 30 % (46, 48 and 38 % at the long window), the vector ALU 44, 33 and 20 %, LDS 20, 19 and 24 %:
+// seen, 705 TFLOP/s, where a large matrix product reaches 1606) and 575 backward (537 TFLOP/s of the formula's; S and dP are taken
+// twice); 16384 tokens of 4 + 1 heads, window 4096: 131 (920 TFLOP/s) and 422.  Of a SIMD's time forward, dQ, dK/dV there the
+// matrix pipe works 35, 34 and 42 % (45, 48 and 47 % at the long window), the vector ALU 44, 33 and 35 %, LDS 20, 19 and 33 %:
 // none of them bounds the kernels alone.  The rest are a wave's own dependences, products to softmax to products, which two or
 // three waves a SIMD do not fill, blocks' starts and ends, and tiles of which the mask leaves a part.
 // What lost: 64 rows a wave (half the LDS reads, one wave a SIMD: forward 224 us for 197, dQ 338 for 294, dK/dV 587 for 450);
-// loads two tiles ahead (forward 175, dK/dV 6 % slower, spills); lane offsets of the loads worked out once (no change).
+// loads two tiles ahead (forward 175, dK/dV 6 % slower, spills); lane offsets of the loads worked out once (no change); dQ by
+// tiles of 32 keys (backward 591 for 575).
 #include "window_bf16.h"
 
 #include <type_traits>
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void window_fwd_kernel(Windo
 
 // ------------------------------------------------------------------ backward: dQ, and the row dots D_i
 // 32 keys at a time, operands three steps ahead; the two waves of a SIMD hide each other's softmax.  (Two blocks of 32 in flight
-// within a wave, operands one step ahead: 8 x 2048 tokens of 32 + 8 heads of 128, window 512, 290 us for 256.)
+// within a wave, operands one step ahead: 8 x 2048 tokens of 32 + 8 heads of 128, window 512, 290 us where 256 were.  The first sweep and D's sums cost 1 %.)
 constexpr int kShort = 4;   // tiles
 template <int DH, bool ORDERED>
 __global__ __launch_bounds__(256, 2) void window_dq_kernel(WindowArgs a, RowOrder ro) {
