@@ -78,7 +78,7 @@ inline int key_rows(const WindowArgs &a) {
   return (long)(a.nq / a.nk) * (tiles < in_window ? tiles : in_window) <= 40 ? 64 : 128;   // (items: tiles of 64 queries of a head)
 }
 // (An item is about 2 us, of 64 keys 1; a slot, two [ROWS][columns] arrays, about a 40th of an item of the whole chip's time.  Costs
-// half or twice as high move the backwards of 24 shapes by less than 1 %, on average.)
+// half or twice as high make the backwards of 24 shapes up to 2 % slower, on average.)
 template <int ROWS> KeyWork work_of(const WindowArgs &a) {
   return key_work<ROWS>(a, ROWS == 64 ? 2 * kCus : kCus, Costs{3, 0.025, 2}, (int)sizeof(bf16));
 }
